@@ -330,6 +330,120 @@ gt_status_t gt_attn_bwd_ring_step(const void* q_shard, const void* o_shard,
                                   int32_t H, int32_t d, gt_dtype_t dtype,
                                   float scale, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Packed batches of graphs of unlike sizes, with capped scores, a prefix mask
+ * and dropout of the probabilities. Graph g has n_q[g] query rows and n_k[g]
+ * keys (the same in training and evaluation; a few new nodes against all the
+ * keys of their graph in serving), its rows packed one graph behind the other.
+ * With u = scale q_i . k_j,
+ *
+ *     c  = cap tanh(u / cap)                 (u where cap is 0)
+ *     S  = c + table[h, spd_g[i, j]]         (bias 0 past n_buckets)
+ *     P  = softmax of S over the keys that row i sees,  LSE its log-sum-exp
+ *     O_i = sum_j P_ij z_ij V_j / (1 - p)
+ *
+ * Row i sees the keys of its own graph (the document mask), and of them
+ *   without a prefix: all; with prefix[g]: those with j < prefix[g] or
+ *   j <= i + n_k[g] - n_q[g] (the last query stands at the last key; prefix 0
+ *   is the causal mask).
+ * Table entries of -1e30 and less are masks, as -inf is. A row that sees no key,
+ * or only masked ones, gets O = 0, LSE = -inf and zero gradient. LSE counts
+ * dropped pairs. V of a key that a row does not see, or only behind a mask,
+ * does not reach the row unless it is NaN or infinite (within one graph 0 times
+ * it is NaN); no value reaches another graph.
+ *
+ * Dropout: z_ij in {0, 1} is never stored but drawn again by every kernel, from
+ * Philox4x32 with 7 rounds: counter (j / 8, packed row of i, head, offset), key
+ * (low, high half of seed). Its words 0..3 hold 16 bits for each of 8 keys, key
+ * j mod 8 = 2 w in the low half of word w and 2 w + 1 in the high half. z = 1 iff
+ * these bits, as a signed integer, are at least t - 32768, t = p 65536 rounded;
+ * 1 / (1 - p) above is 65536 / (65536 - t). The same (seed, offset) gives the same z
+ * whatever the other graphs of a plan's later rows are; layers, steps and ranks
+ * take offsets or seeds of their own.
+ *
+ * Tensors of rows: element (h, row, c) at p + h head_stride + row row_stride + c,
+ * strides in elements, so [H, rows, d] and [rows, H, d] layouts are taken as they
+ * are. p 16-byte aligned, strides multiples of 16 bytes, row_stride from d to
+ * 2^23. Rows from the batch's total on are neither read nor written. */
+typedef struct {
+  void* p;
+  int64_t head_stride, row_stride;
+} gt_attn_rows_t;
+
+/* A plan's sizes, filled by gt_attn_pack_plan; read only for the caller. */
+typedef struct {
+  int64_t total_q, total_k;    /* packed rows of all graphs */
+  int64_t spd_bytes;           /* bytes of distances that the batch reads from */
+  int64_t plan_bytes;
+  int32_t n_graphs, H;
+  /* internal: the kernels' work lists inside the plan */
+  int32_t jobs[3], merges, parts, reserved;
+  int64_t job_off[3], group_off[3], merge_off;
+} gt_attn_pack_t;
+
+typedef struct {
+  double p;                    /* 0 <= p < 1 - 2^-17 */
+  uint64_t seed;
+  uint32_t offset;
+  const uint32_t* offset_dev;  /* NULL, or device memory whose value is added to offset
+                                  (mod 2^32) when the kernels run: a captured graph's
+                                  replays advance it */
+} gt_attn_dropout_t;
+
+/* Plan of a packed batch (host code, nothing is launched): the work lists of the
+ * kernels below for these sizes and H heads.
+ *   n_q, n_k  [n_graphs] rows, 0 allowed, at most 2^25 - 16
+ *   prefix    [n_graphs] >= 0, or NULL: no prefix mask
+ *   spd_off, spd_ld  [n_graphs] byte offset of a graph's [n_q, n_k] distances and
+ *             their row stride (n_k .. 2^25 - 16), or NULL: the matrices lie dense, one
+ *             behind the other
+ *   plan      NULL: only *info is filled; else host memory of plan_bytes bytes that
+ *             receives the plan, which the caller copies to device memory (16-byte
+ *             aligned) and passes to the calls as it is.
+ * GT_ERR_WORKSPACE: plan_bytes is below info->plan_bytes (*info is filled), or no
+ * host memory. All arrays are HOST arrays. */
+gt_status_t gt_attn_pack_plan(int32_t n_graphs, int32_t H, const int32_t* n_q, const int32_t* n_k,
+                              const int32_t* prefix, const int64_t* spd_off, const int64_t* spd_ld,
+                              void* plan, size_t plan_bytes, gt_attn_pack_t* info);
+
+/* Bytes of device workspace (256-byte aligned; contents ignored) of the two
+ * calls; 0 for a forward that needs none. */
+size_t gt_attn_pack_fwd_workspace_size(const gt_attn_pack_t* pack, int32_t d);
+size_t gt_attn_pack_bwd_workspace_size(const gt_attn_pack_t* pack, int32_t n_buckets);
+
+/* Forward.
+ *   pack, plan  from gt_attn_pack_plan (plan: its copy on the device)
+ *   q [H, >= total_q, d], k, v [H, >= total_k, d] dtype; o as q (written)
+ *   spd    >= pack->spd_bytes bytes    table [H, n_buckets] fp32
+ *   lse    [H, ld_lse] fp32 (written), ld_lse >= total_q
+ *   cap    0 (no cap), or positive and finite
+ *   dropout NULL: none
+ * Otherwise as gt_attn_fwd. Deterministic. */
+gt_status_t gt_attn_pack_fwd(const gt_attn_pack_t* pack, const void* plan, const gt_attn_rows_t* q,
+                             const gt_attn_rows_t* k, const gt_attn_rows_t* v, const uint8_t* spd,
+                             const float* table, int32_t n_buckets, const gt_attn_rows_t* o, float* lse,
+                             int64_t ld_lse, void* workspace, size_t workspace_bytes, int32_t d,
+                             gt_dtype_t dtype, float scale, float cap, const gt_attn_dropout_t* dropout,
+                             void* stream);
+
+/* Backward of L = sum(O * dO), with the forward's arguments and results:
+ *   dP = z (dO V^T) / (1 - p),  dS = P (dP - rowsum(dO * O)),
+ *   dV = (P z)^T dO / (1 - p),  dU = dS (1 - tanh^2(u / cap)),
+ *   dQ = scale dU K,  dK = scale dU^T Q,
+ *   dtable[h, b] = sum of dS over pairs with spd == b
+ *   dq as q, dk, dv as k (overwritten); dtable [H, n_buckets] fp32 (overwritten).
+ * The table gradient is exact to fp32 for bf16 inputs too (the row sums are
+ * corrected for the rounding of O). If a dS of a head is no finite number, its whole
+ * dtable row is NaN. Deterministic, the table gradient included. */
+gt_status_t gt_attn_pack_bwd(const gt_attn_pack_t* pack, const void* plan, const gt_attn_rows_t* q,
+                             const gt_attn_rows_t* k, const gt_attn_rows_t* v, const uint8_t* spd,
+                             const float* table, int32_t n_buckets, const gt_attn_rows_t* o,
+                             const float* lse, int64_t ld_lse, const gt_attn_rows_t* d_o,
+                             const gt_attn_rows_t* dq, const gt_attn_rows_t* dk, const gt_attn_rows_t* dv,
+                             float* dtable, void* workspace, size_t workspace_bytes, int32_t d,
+                             gt_dtype_t dtype, float scale, float cap, const gt_attn_dropout_t* dropout,
+                             void* stream);
+
 /* Static, human-readable name of a status code. */
 const char* gt_status_string(gt_status_t s);
 

@@ -23,3 +23,9 @@ from .attention import (  # noqa: F401
     ring_backward_super,
     lse_bias_only,
 )
+from .packed import (  # noqa: F401
+    keep_mask,
+    packed_backward,
+    packed_forward,
+    philox4x32,
+)

@@ -15,6 +15,10 @@ If the library is missing or cannot be loaded, every call raises.
     gt_attn_ring_step_acc(q_sh, k_sh, v_sh, spd_shard, row_off, col_off, table, state)
     dq, dk, dv, dt = gt_attn_bwd_ring_step(q_sh, o_sh, lse_sh, do_sh, k_blk, v_blk, spd_shard,
                                            row_off, col_off, table, acc=(dq, dk, dv, dt))
+    pack = gt_attn_pack(sizes, H)                       # graphs of unlike sizes, packed: see packed.py
+    o, lse = gt_attn_pack_fwd(q, k, v, spd, table, pack, cap=30.0, dropout=GTDropout(0.1, seed))
+    dq, dk, dv, dtable = gt_attn_pack_bwd(q, k, v, spd, table, pack, o, lse, d_o, cap=30.0,
+                                          dropout=GTDropout(0.1, seed))
 """
 from __future__ import annotations
 
@@ -28,6 +32,8 @@ __all__ = ["gt_attn_fwd", "gt_attn_bwd", "gt_attn_bwd_phase", "gt_attn_bwd_noall
            "gt_attn_bwd_noalloc_max_bytes", "gt_attn_ring_step",
            "gt_attn_ring_step_acc", "gt_attn_merge",
            "gt_attn_bwd_ring_step", "gt_attn_bwd_workspace_size", "gt_attn_bwd_ring_workspace_size",
+           "gt_attn_pack", "gt_attn_pack_fwd", "gt_attn_pack_bwd", "gt_attn_pack_fwd_workspace_size",
+           "gt_attn_pack_bwd_workspace_size", "GTDropout", "GTPack",
            "gt_status_string", "gt_attn_version",
            "GTError", "lib", "LIB_PATH"]
 
@@ -93,6 +99,7 @@ def lib() -> ctypes.CDLL:
                                             _I32, _I32, _I32, _F, _P]
         L.gt_attn_merge.restype = _I32
         L.gt_attn_merge.argtypes = [_P, _P, _I32, _P, _P, _I32, _I64, _I32, _I32, _P]
+        packed._register(L)
         L.gt_status_string.restype = ctypes.c_char_p
         L.gt_status_string.argtypes = [_I32]
         L.gt_attn_version.restype = _I32
@@ -558,3 +565,8 @@ def gt_attn_merge(o_parts, lse_parts, dtype=torch.bfloat16, out=None, lse=None, 
                              GT_BF16 if out.dtype == torch.bfloat16 else GT_F32, _stream(stream))
     _check(st, "gt_attn_merge")
     return out, lse
+
+
+from . import packed  # noqa: E402  (it takes the helpers above)
+from .packed import (GTDropout, GTPack, gt_attn_pack, gt_attn_pack_bwd,  # noqa: E402
+                     gt_attn_pack_bwd_workspace_size, gt_attn_pack_fwd, gt_attn_pack_fwd_workspace_size)

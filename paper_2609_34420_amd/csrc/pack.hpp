@@ -1,0 +1,406 @@
+// Building blocks of the packed kernels (pack_fwd.hpp, pack_dq.hpp,
+// pack_dkdv.hpp): attention over a packed batch of graphs with capped scores,
+// a prefix mask and dropout.
+//
+//   u_ij = scale q_i . k_j,   c_ij = cap tanh(u_ij / cap)   (u_ij without a cap)
+//   S_ij = c_ij + table[h, spd_ij]
+//   key j is visible to query i of its graph if j < max(prefix, i + nk - nq + 1)
+//   P = softmax of S over the visible keys,   O_i = sum_j P_ij z_ij V_j / (1 - p)
+// with z_ij in {0, 1} drawn by Philox4x32 (below) in every kernel that needs it.
+//
+// Layout. A wave has 32 stationary rows (lane & 31) and computes 32 x 32 score
+// blocks whose streamed rows lie on the registers: lane half g (lane >> 5) holds
+// streamed rows 16 g + r in register r, in the order that the next product
+// takes them (perm32). Two policies give the products and the staging: Bf16Pack
+// (v_mfma_f32_32x32x16_bf16) and F32Pack (v_mfma_f32_32x32x2_f32).
+//
+// Two workgroups of 4 waves per compute unit, each with one staged tile; the
+// next tile's rows are in flight in registers meanwhile.
+#pragma once
+#include <type_traits>
+
+#include "common.hpp"
+#include "f32_mfma.hpp"
+#include "pack_plan.hpp"
+#include "stage.hpp"
+
+namespace gt {
+
+// A tensor of heads x rows x d with unit feature stride (strides in elements).
+struct PackTensor {
+  void* p;
+  int64_t hs, rs;
+};
+
+struct PackArgs {
+  PackTensor q, k, v, o, d_o, dq, dk, dv;
+  float* lse;               // [H, ld_lse]
+  int64_t ld_lse;
+  const uint8_t* spd;
+  const float* table;       // [H, n_buckets]
+  int32_t n_buckets, H;
+  float scale, cap;
+  int32_t thr;              // pairs whose signed 16 random bits are below it are dropped
+  float rp;                 // 1 / (1 - p)
+  uint32_t seed0, seed1, offset;
+  const uint32_t* offset_dev;   // added to offset, or null
+  const PackJob* jobs;
+  const PackGroup* groups;
+  int32_t njobs;
+  const PackMerge* merges;
+  int32_t nmerges;
+  float* o_part;            // [slot, H, 32, d]
+  float* lse_part;          // [slot, H, 32]
+  float* dlt;               // [H, ld_dlt] rowsum(dO * O)
+  int64_t ld_dlt;
+  float2* dmax;             // [H, njobs_dq * 4] of each wave of the dQ kernel: largest |dS|, and
+                            // largest correction of a row's D
+  int32_t njobs_dq;
+  double* dtab_part;        // [H, njobs, n_buckets]
+  float* dtable;            // [H, n_buckets]
+};
+
+namespace {
+
+constexpr int kPackThreads = kPackWaves * 64;
+constexpr float kNoScore = -1e30f;        // table entries at or below it are masks, as -inf
+
+// ---------------------------------------------------------------------------
+// Philox4x32 with 7 rounds (Salmon et al., Parallel random numbers: as easy as
+// 1, 2, 3, 2011: the fewest rounds that pass their whole battery; 10 is their
+// margin). Counter (key / 8, packed query row, head, offset), key = seed: one
+// draw gives the 8 keys of a row from a multiple of 8 on 16 bits each, key 2 w
+// in the low half of word w. 16 bits place p within 2^-17, and the kept pairs
+// are scaled by the exact inverse of the rate so placed.
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ uint4 philox7(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0, uint32_t k1) {
+#pragma unroll
+  for (int i = 0; i < 7; ++i) {
+    const uint64_t x = (uint64_t)c0 * 0xD2511F53u, y = (uint64_t)c2 * 0xCD9E8D57u;
+    c0 = (uint32_t)(y >> 32) ^ c1 ^ k0;
+    c2 = (uint32_t)(x >> 32) ^ c3 ^ k1;
+    c1 = (uint32_t)y;
+    c3 = (uint32_t)x;
+    k0 += 0x9E3779B9u;
+    k1 += 0xBB67AE85u;
+  }
+  return make_uint4(c0, c1, c2, c3);
+}
+
+// The random halves of 16 consecutive keys of packed row `row` from key j (a
+// multiple of 16) on: word w holds keys j + 2 w (low) and j + 2 w + 1.
+__device__ __forceinline__ void draw16(const PackArgs& a, uint32_t offset, int h, uint32_t row, int j, uint32_t (&w)[8]) {
+  const uint4 x = philox7((uint32_t)(j >> 3), row, (uint32_t)h, offset, a.seed0, a.seed1);
+  const uint4 y = philox7((uint32_t)(j >> 3) + 1u, row, (uint32_t)h, offset, a.seed0, a.seed1);
+  w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+  w[4] = y.x; w[5] = y.y; w[6] = y.z; w[7] = y.w;
+}
+__device__ __forceinline__ bool kept(const uint32_t (&w)[8], int r, int thr) {
+  return (int)(int16_t)(w[r >> 1] >> (16 * (r & 1))) >= thr;
+}
+
+// ---------------------------------------------------------------------------
+// Scores. Units: bf16 works in base 2 (x = S log2 e), fp32 in S itself.
+// ---------------------------------------------------------------------------
+struct ScoreConst {
+  float mul, add;           // bf16, capped: e = 2^(s mul) = e^(2 u / cap), x = add / (e + 1) + bias
+  float cap;                // fp32
+};
+
+// D: the tile's head dim (32 or 64); DS <= D: the tensors'.
+template <int D_, int DS_>
+struct Bf16Pack {
+  static constexpr int D = D_, DS = DS_;
+  static constexpr bool BF16 = true;
+  using T = uint16_t;
+  static constexpr int NA = D / 32;                  // accumulators of D x 32
+  static constexpr int TILE = 32 * D;                // elements of a wave's staged rows
+  static constexpr int CPR = D / 8;                  // 16-byte chunks per row
+  static constexpr int DCH = DS / 8;                 // of them with data
+  struct Operand { bf16x8 f[D / 16]; };
+
+  __device__ __forceinline__ static int lds_off(int row, int ch) { return row * D + swz_tile<D>(row, ch) * 8; }
+
+  // The lane's stationary row (features past DS zero).
+  __device__ __forceinline__ static void load_operand(const T* row, bool ok, float, Operand& x) {
+    const int g = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int kc = 0; kc < D / 16; ++kc)
+      x.f[kc] = ok && kc * 16 + g * 8 < DS ? *reinterpret_cast<const bf16x8*>(row + kc * 16 + g * 8) : zero_bf16x8();
+  }
+  // Dot product of two operands' features in this lane half.
+  __device__ __forceinline__ static float dot(const Operand& x, const Operand& y) {
+    float s = 0.0f;
+#pragma unroll
+    for (int kc = 0; kc < (DS + 15) / 16; ++kc)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s = fmaf((float)x.f[kc][e], (float)y.f[kc][e], s);
+    return s;
+  }
+  __device__ __forceinline__ static void rows(const T* tile, const Operand& x, f32x16& s) {
+#pragma unroll
+    for (int kc = 0; kc < (DS + 15) / 16; ++kc) s = mfma32(lds_b128(tile + row_operand_off<D>(kc)), x.f[kc], s);
+  }
+  __device__ __forceinline__ static void cols(const T* tile, const bf16x8& p0, const bf16x8& p1, f32x16 (&acc)[NA]) {
+#pragma unroll
+    for (int cb = 0; cb < NA; ++cb) {
+      const int o0 = tr_operand_off<D>(0, cb), o1 = tr_operand_off<D>(1, cb);
+      acc[cb] = mfma32(lds_tr_operand(tile, o0, o1), p0, acc[cb]);
+      acc[cb] = mfma32(lds_tr_operand(tile + 8 * D, o0, o1), p1, acc[cb]);
+    }
+  }
+  __device__ __forceinline__ static void cols(const T* tile, const float (&p)[16], f32x16 (&acc)[NA]) {
+    cols(tile, cvt_bf16x8(p), cvt_bf16x8(p + 8), acc);
+  }
+  // put(feature, 4 values) for the lane's column.
+  template <typename F>
+  __device__ __forceinline__ static void features(const f32x16 (&acc)[NA], F put) {
+    const int g = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int cb = 0; cb < NA; ++cb)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int c = cb * 32 + 8 * u + 4 * g;
+        if (c < DS) put(c, make_float4(acc[cb][4 * u], acc[cb][4 * u + 1], acc[cb][4 * u + 2], acc[cb][4 * u + 3]));
+      }
+  }
+  __device__ __forceinline__ static void store4(T* p, float4 v) {
+    uint2 pk;
+    pk.x = (uint32_t)f2bf(v.x) | ((uint32_t)f2bf(v.y) << 16);
+    pk.y = (uint32_t)f2bf(v.z) | ((uint32_t)f2bf(v.w) << 16);
+    *reinterpret_cast<uint2*>(p) = pk;
+  }
+
+  __device__ __forceinline__ static float operand_mul(const PackArgs&, bool) { return 1.0f; }
+  __device__ __forceinline__ static ScoreConst consts(const PackArgs& a, bool cap) {
+    ScoreConst c;
+    c.mul = a.scale * kLog2e * (cap ? 2.0f / a.cap : 1.0f);
+    c.add = -2.0f * a.cap * kLog2e;
+    c.cap = a.cap;
+    return c;
+  }
+  // Table entry in LDS: bias log2 e, and with a cap its log2 e too, since
+  // cap tanh(u / cap) = cap - 2 cap / (e^(2 u / cap) + 1).
+  __device__ __forceinline__ static float entry(float bias, const PackArgs& a, bool cap) {
+    return bias <= kNoScore ? -INFINITY : bias * kLog2e + (cap ? a.cap * kLog2e : 0.0f);
+  }
+  // Score from the product s; slope: dc/du (times 1/4 with a cap, see kSlope).
+  static constexpr float kSlope = 4.0f;
+  template <bool CAP>
+  __device__ __forceinline__ static float score(float s, float bias, const ScoreConst& c, float& slope) {
+    if constexpr (!CAP) return fmaf(s, c.mul, bias);
+    const float r = __builtin_amdgcn_rcpf(exp2_fast(s * c.mul) + 1.0f);
+    slope = fmaf(-r, r, r);                          // 1 - tanh^2 = 4 (r - r^2)
+    return fmaf(r, c.add, bias);
+  }
+  __device__ __forceinline__ static float expo(float x, float mneg) { return exp2_fast(x + mneg); }
+  __device__ __forceinline__ static float to_unit(float lse) { return lse * kLog2e; }
+  __device__ __forceinline__ static float log_sum(float m, float l) { return (m + __log2f(l)) * kLn2; }
+};
+
+template <int D_>
+struct F32Pack {
+  static constexpr int D = D_, DS = D_;
+  static constexpr bool BF16 = false;
+  using T = float;
+  static constexpr int NA = kBlocksF<D>;
+  static constexpr int TILE = 32 * kRowF<D>;
+  static constexpr int CPR = D / 4;
+  static constexpr int DCH = CPR;
+  struct Operand { float f[D / 2]; };
+
+  __device__ __forceinline__ static int lds_off(int row, int ch) { return row * kRowF<D> + ch * 4; }
+  __device__ __forceinline__ static void load_operand(const T* row, bool ok, float mul, Operand& x) {
+    const int g = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int c = 0; c < D / 8; ++c) {
+      const float4 v = ok ? *reinterpret_cast<const float4*>(row + 8 * c + 4 * g) : make_float4(0.f, 0.f, 0.f, 0.f);
+      x.f[4 * c] = v.x * mul;
+      x.f[4 * c + 1] = v.y * mul;
+      x.f[4 * c + 2] = v.z * mul;
+      x.f[4 * c + 3] = v.w * mul;
+    }
+  }
+  __device__ __forceinline__ static float dot(const Operand& x, const Operand& y) {
+    float s = 0.0f;
+#pragma unroll
+    for (int e = 0; e < D / 2; ++e) s = fmaf(x.f[e], y.f[e], s);
+    return s;
+  }
+  __device__ __forceinline__ static void rows(const T* tile, const Operand& x, f32x16& s) {
+    product_rows<D>(tile, x.f, s);
+  }
+  __device__ __forceinline__ static void cols(const T* tile, const float (&p)[16], f32x16 (&acc)[NA]) {
+    product_cols<D>(tile, p, acc);
+  }
+  template <typename F>
+  __device__ __forceinline__ static void features(const f32x16 (&acc)[NA], F put) { for_features<D>(acc, put); }
+  __device__ __forceinline__ static void store4(T* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
+
+  // The stationary operand of the score product carries scale (/ cap).
+  __device__ __forceinline__ static float operand_mul(const PackArgs& a, bool cap) {
+    return cap ? a.scale / a.cap : a.scale;
+  }
+  __device__ __forceinline__ static ScoreConst consts(const PackArgs& a, bool) { return {1.0f, 0.0f, a.cap}; }
+  __device__ __forceinline__ static float entry(float bias, const PackArgs&, bool) {
+    return bias <= kNoScore ? -INFINITY : bias;
+  }
+  static constexpr float kSlope = 1.0f;
+  // tanh by its series up to 0.3 (next term 5e-8 of it), else 1 - 2 / (e^(2 y) + 1),
+  // off by about 2^-23 against a value of at least 0.29.
+  template <bool CAP>
+  __device__ __forceinline__ static float score(float y, float bias, const ScoreConst& c, float& slope) {
+    if constexpr (!CAP) return y + bias;
+    const float y2 = y * y;
+    const float small = y * fmaf(y2, fmaf(y2, fmaf(y2, fmaf(y2, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f),
+                                          -1.0f / 3.0f), 1.0f);
+    const float big = fmaf(-2.0f, 1.0f / (exp2_fast(fabsf(y) * (2.0f * kLog2e)) + 1.0f), 1.0f);
+    const float t = fabsf(y) < 0.3f ? small : copysignf(big, y);
+    slope = fmaf(-t, t, 1.0f);
+    return fmaf(c.cap, t, bias);
+  }
+  __device__ __forceinline__ static float expo(float x, float mneg) { return exp2_fast((x + mneg) * kLog2e); }
+  __device__ __forceinline__ static float to_unit(float lse) { return lse; }
+  __device__ __forceinline__ static float log_sum(float m, float l) { return m + logf(l); }
+};
+
+// ---------------------------------------------------------------------------
+// Staging: 32 rows of one tensor per wave, global -> registers -> LDS.
+// ---------------------------------------------------------------------------
+template <class M>
+struct PackStage {
+  static constexpr int N = 32 * M::CPR / 64;         // 16-byte chunks per lane
+  uint4 r[N];
+  // Rows [r0, r0 + 32) of a graph's `rows` rows from p on (rows past them zero).
+  __device__ __forceinline__ void load(const typename M::T* p, int64_t rs, int64_t r0, int64_t rows) {
+    constexpr int ES = sizeof(typename M::T);
+    const int64_t n = rows - r0 < 32 ? rows - r0 : 32;
+    const uint32_t rsb = (uint32_t)rs * ES;
+    const __amdgpu_buffer_rsrc_t rc = make_rsrc_n(p + r0 * rs, n > 0 ? (n - 1) * (int64_t)rsb + M::DS * ES : 0);
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int u = i * 64 + lane, row = u / M::CPR, ch = u % M::CPR;
+      r[i] = buf_b128(rc, ch < M::DCH ? (uint32_t)row * rsb + (uint32_t)ch * 16u : kZeroChunk);
+    }
+  }
+  __device__ __forceinline__ void store(typename M::T* tile) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int u = i * 64 + lane;
+      opaque(r[i]);
+      *reinterpret_cast<uint4*>(tile + M::lds_off(u / M::CPR, u % M::CPR)) = r[i];
+    }
+  }
+};
+
+// The workgroup's job and head, the wave's group. Workgroups go to the 8 XCDs
+// round robin: with many jobs, a job's heads, which share its distances, stay on
+// one XCD, and the jobs, longest first, are dealt over the XCDs in turn.
+constexpr int kXcdJobs = 64;
+__host__ __device__ inline unsigned pack_grid(int njobs, int H) {
+  return njobs >= kXcdJobs ? (unsigned)((njobs + 7) / 8 * 8) * (unsigned)H : (unsigned)njobs * (unsigned)H;
+}
+struct PackPlace {
+  int job, h;
+  __device__ __forceinline__ explicit PackPlace(const PackArgs& a) {
+    const int w = (int)blockIdx.x;
+    if (a.njobs >= kXcdJobs) {
+      const int i = w >> 3;
+      h = i % a.H;
+      job = i / a.H * 8 + (w & 7);
+    } else {
+      h = w % a.H;
+      job = w / a.H;
+    }
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ T* rows_at(const PackTensor& t, int h, int64_t row) {
+  return reinterpret_cast<T*>(t.p) + h * t.hs + row * t.rs;
+}
+
+// The distances of a query-stationary wave: the lane's row, groups of 16 keys
+// from key j (wave-uniform) + 16 g on, at any address.
+struct PackSpdRow {
+  const uint8_t* base;
+  int range;
+  uint32_t voff, sh;
+  // first: the wave's first row; rows: the query rows from there on (at least 1).
+  __device__ __forceinline__ PackSpdRow(const uint8_t* first, int64_t ld, int64_t rows, int nk) {
+    const int lane = threadIdx.x & 63;
+    const int64_t n = rows < 32 ? rows : 32;
+    const uint32_t rem = (uint32_t)(reinterpret_cast<uintptr_t>(first) & 15u);
+    const int64_t i = (lane & 31) < n ? (lane & 31) : n - 1;
+    base = first - rem;
+    range = rsrc_range(((n - 1) * ld + nk + rem + 3) & ~(int64_t)3);
+    voff = (uint32_t)(i * ld) + 16u * (uint32_t)(lane >> 5) + rem;
+    sh = voff & 3u;
+    voff -= sh;
+  }
+  __device__ __forceinline__ void fetch(int j, uint32_t (&w)[5]) const {
+    load_spd5(make_rsrc_from(base, range, j), voff, w);
+  }
+};
+
+// Bias entries of the lane's 16 distances.
+__device__ __forceinline__ void bias16(const float* tab, const uint32_t* w, float (&b)[16]) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) b[r] = tab[(w[r >> 2] >> (8 * (r & 3))) & 0xffu];
+}
+
+// Adds up the accumulators of groups that have the same rows (wave gw of group
+// ks into wave gw of group 0), pairwise and in a fixed order. buf: two waves'
+// accumulators. on_write(slot) and weights(slot, wa, wo) as in combine_groups.
+template <int NA, typename W, typename R>
+__device__ __forceinline__ void pack_combine(float* buf, int log2w, int ks, int gw, f32x16 (&acc)[NA], W on_write, R weights) {
+  constexpr int XW = NA * 16 * 64;
+  const int lane = threadIdx.x & 63;
+  for (int half = (kPackWaves >> log2w) / 2; half >= 1; half >>= 1) {
+    __syncthreads();
+    if (ks >= half && ks < 2 * half) {
+      const int slot = ((ks - half) << log2w) + gw;
+      float4* x = reinterpret_cast<float4*>(buf + slot * XW) + lane;
+      on_write(slot);
+#pragma unroll
+      for (int c = 0; c < NA; ++c)
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          x[(c * 4 + u) * 64] = make_float4(acc[c][4 * u], acc[c][4 * u + 1], acc[c][4 * u + 2], acc[c][4 * u + 3]);
+    }
+    __syncthreads();
+    if (ks < half) {
+      const int slot = (ks << log2w) + gw;
+      const float4* x = reinterpret_cast<const float4*>(buf + slot * XW) + lane;
+      float wa, wo;
+      weights(slot, wa, wo);
+#pragma unroll
+      for (int c = 0; c < NA; ++c)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const float4 y = x[(c * 4 + u) * 64];
+          acc[c][4 * u] = fmaf(acc[c][4 * u], wa, y.x * wo);
+          acc[c][4 * u + 1] = fmaf(acc[c][4 * u + 1], wa, y.y * wo);
+          acc[c][4 * u + 2] = fmaf(acc[c][4 * u + 2], wa, y.z * wo);
+          acc[c][4 * u + 3] = fmaf(acc[c][4 * u + 3], wa, y.w * wo);
+        }
+    }
+  }
+}
+
+}  // namespace
+
+// Launchers (hipError_t of the launch). BF16 inputs of head dim d, with or
+// without a cap and dropout.
+hipError_t launch_pack_fwd_bf16(const PackArgs& a, int d, bool cap, bool drop, hipStream_t s);
+hipError_t launch_pack_fwd_f32(const PackArgs& a, int d, bool cap, bool drop, hipStream_t s);
+hipError_t launch_pack_dq_bf16(const PackArgs& a, int d, bool cap, bool drop, hipStream_t s);
+hipError_t launch_pack_dq_f32(const PackArgs& a, int d, bool cap, bool drop, hipStream_t s);
+hipError_t launch_pack_dkdv_bf16(const PackArgs& a, int d, bool cap, bool drop, hipStream_t s);
+hipError_t launch_pack_dkdv_f32(const PackArgs& a, int d, bool cap, bool drop, hipStream_t s);
+hipError_t launch_pack_merge(const PackArgs& a, int d, bool bf16, hipStream_t s);
+hipError_t launch_pack_dtable(const PackArgs& a, hipStream_t s);
+
+}  // namespace gt

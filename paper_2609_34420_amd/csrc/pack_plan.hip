@@ -1,0 +1,249 @@
+// Plan of a packed batch of graphs: which rows and columns each workgroup of
+// the packed kernels takes. Host code only; the plan depends on the sizes, the
+// prefixes and the number of heads.
+//
+// Rows are dealt out in blocks of 32 per wave. Where the batch fills the chip, a
+// graph of more than 64 rows gives workgroups of 128 rows, and smaller ones
+// share a workgroup, 2 or 4 of them (those with the most alike numbers of
+// columns together, since a workgroup's waves meet at every tile). Where it does
+// not, 2 or 4 groups of waves take the same rows and a part of the columns each,
+// and in the forward with few rows against many keys several workgroups do, whose
+// partial results are merged by a kernel of its own.
+#include <algorithm>
+#include <cstring>
+#include <limits>
+#include <vector>
+
+#include "../../include/gt_attn.h"
+#include "pack_plan.hpp"
+
+namespace gt {
+namespace {
+
+constexpr int64_t kMaxNodes = (1LL << 25) - 16;   // 32 rows of distances stay below 2^31 bytes
+constexpr int kSlots = 512;                       // workgroups that run at a time: two per compute unit
+constexpr int kSetup = 3;                         // cost of a workgroup's start and end, in 32 x 32 blocks
+
+enum Stage { kForward, kDq, kDkdv };
+
+struct Graph {
+  int32_t q0, nq, k0, nk, prefix, ld;
+  int64_t spd;
+};
+
+struct Plan {
+  std::vector<PackGroup> groups;
+  std::vector<PackJob> jobs;
+  std::vector<PackMerge> merges;
+  int32_t parts = 0;
+};
+
+int32_t clamp32(int64_t x, int64_t lo, int64_t hi) { return (int32_t)std::min(std::max(x, lo), hi); }
+
+// Columns that rows [row0, row0 + rows) of a graph meet.
+void columns(const Graph& g, Stage st, int32_t row0, int32_t rows, int32_t& c0, int32_t& c1) {
+  const int64_t off = (int64_t)g.nk - g.nq;
+  if (st != kDkdv) {
+    const int64_t last = std::min<int64_t>(g.nq, (int64_t)row0 + rows) - 1;
+    c0 = 0;
+    c1 = clamp32(std::max<int64_t>(g.prefix, last + off + 1), 0, g.nk);
+  } else {
+    c0 = row0 < g.prefix ? 0 : clamp32(row0 - off, 0, g.nq) / 32 * 32;
+    c1 = g.nq;
+  }
+}
+
+struct Item {
+  PackGroup g;
+  int32_t cost;       // blocks per wave
+};
+
+// The jobs of one stage with 128 / s rows per workgroup (s = 1, 2, 4).
+Plan build(const std::vector<Graph>& graphs, int32_t H, Stage st, int s) {
+  Plan p;
+  std::vector<std::vector<Item>> whole(3);         // by log2w: groups that share a workgroup with others
+  std::vector<std::pair<int32_t, PackJob>> jobs;   // cost, job
+  std::vector<std::pair<Item, int>> split;         // combined: item, log2w
+  for (const Graph& g : graphs) {
+    const int32_t rows = st == kDkdv ? g.nk : g.nq;
+    int lw = s == 1 ? 2 : (s == 2 ? 1 : 0);
+    while (lw > 0 && rows <= (32 << (lw - 1))) --lw;
+    const int32_t step = 32 << lw;
+    for (int64_t r = 0; r < rows; r += step) {
+      Item it{};
+      it.g = PackGroup{g.q0, g.nq, g.k0, g.nk, (int32_t)r, 0, 0, g.prefix, g.spd, g.ld, -1};
+      columns(g, st, (int32_t)r, step, it.g.c0, it.g.c1);
+      it.cost = (it.g.c1 - it.g.c0 + 31) / 32;
+      if (s == 1)
+        whole[lw].push_back(it);
+      else
+        split.push_back({it, lw});
+    }
+  }
+  for (int lw = 0; lw < 3; ++lw) {
+    auto& w = whole[lw];
+    std::stable_sort(w.begin(), w.end(), [](const Item& a, const Item& b) { return a.cost > b.cost; });
+    const int n = kPackWaves >> lw;
+    for (size_t i = 0; i < w.size(); i += n) {
+      PackJob j{(int32_t)p.groups.size(), lw, 0, (w[i].cost + (1 << lw) - 1) >> lw};
+      for (int k = 0; k < n; ++k)
+        p.groups.push_back(i + k < w.size() ? w[i + k].g : PackGroup{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, -1});
+      jobs.push_back({w[i].cost, j});
+    }
+  }
+  // Parts: with 32-row workgroups that still leave the chip empty, as many per
+  // item as make all about equally long.
+  int32_t target = std::numeric_limits<int32_t>::max();
+  if (st == kForward && s == 4) {
+    int64_t sum = 0;
+    int32_t top = 0;
+    for (auto& it : split) {
+      sum += it.first.cost;
+      top = std::max(top, it.first.cost);
+    }
+    const int64_t even = std::max<int64_t>(16, (sum * H + kSlots - 1) / kSlots);
+    // (a merge costs a launch, about 8 blocks: 4 waves share an item's blocks)
+    if ((int64_t)split.size() * H < kSlots && top / 4 > even / 4 + 8) target = (int32_t)even;
+  }
+  for (auto& e : split) {
+    const Item& it = e.first;
+    const int lw = e.second, n = kPackWaves >> lw;
+    const int32_t unit = n * (32 << lw);             // columns per step of a combined workgroup
+    const int32_t cols = it.g.c1 - it.g.c0;
+    int32_t parts = 1;
+    if (it.cost > target) parts = std::min((it.cost + target - 1) / target, (cols + unit - 1) / unit);
+    int32_t per_part = (cols + parts - 1) / std::max(parts, 1);
+    per_part = (per_part + unit - 1) / unit * unit;
+    parts = per_part > 0 ? std::max(1, (cols + per_part - 1) / per_part) : 1;
+    if (parts > 1) {
+      p.merges.push_back({it.g.q0 + it.g.row0, std::min(32 << lw, it.g.nq - it.g.row0), p.parts, parts});
+    }
+    for (int32_t k = 0; k < parts; ++k) {
+      const int32_t a = it.g.c0 + k * per_part, b = parts == 1 ? it.g.c1 : std::min(it.g.c1, a + per_part);
+      int32_t per = ((b - a + n - 1) / n + (32 << lw) - 1) / (32 << lw) * (32 << lw);
+      PackJob j{(int32_t)p.groups.size(), lw, n > 1 ? 1 : 0, per / (32 << lw)};
+      for (int i = 0; i < n; ++i) {
+        PackGroup g = it.g;
+        g.c0 = (int32_t)std::min<int64_t>(a + (int64_t)i * per, b > a ? (b + 31) / 32 * 32 : a);
+        g.c1 = (int32_t)std::max<int64_t>(g.c0, std::min<int64_t>(a + (int64_t)(i + 1) * per, b));
+        g.part = parts > 1 ? p.parts : -1;
+        p.groups.push_back(g);
+      }
+      if (parts > 1) ++p.parts;
+      jobs.push_back({per / 32, j});
+    }
+  }
+  std::stable_sort(jobs.begin(), jobs.end(),
+                   [](const std::pair<int32_t, PackJob>& a, const std::pair<int32_t, PackJob>& b) {
+                     return a.first > b.first;
+                   });
+  for (auto& j : jobs) p.jobs.push_back(j.second);
+  return p;
+}
+
+// The longest workgroup, or the chip's share of all of them.
+double span(const Plan& p, int32_t H) {
+  double sum = 0.0, top = 0.0;
+  for (const PackJob& j : p.jobs) {
+    const double c = (double)j.steps * (1 << j.log2w) + kSetup;
+    sum += c;
+    top = std::max(top, c);
+  }
+  return std::max(sum * H / kSlots, top) + (p.parts ? 8.0 : 0.0);
+}
+
+Plan best_plan(const std::vector<Graph>& graphs, int32_t H, Stage st) {
+  Plan best = build(graphs, H, st, 1);
+  double cost = span(best, H);
+  for (int s = 2; s <= 4; s *= 2) {
+    Plan p = build(graphs, H, st, s);
+    const double c = span(p, H);
+    if (c < 0.95 * cost) {
+      cost = c;
+      best = std::move(p);
+    }
+  }
+  return best;
+}
+
+template <typename T>
+int64_t place(size_t& at, const std::vector<T>& v, uint8_t* buf) {
+  const size_t off = at;
+  const size_t n = v.size() * sizeof(T);
+  if (buf && n) std::memcpy(buf + off, v.data(), n);
+  at = (off + n + 255) / 256 * 256;
+  return (int64_t)off;
+}
+
+gt_status_t make(int32_t G, int32_t H, const int32_t* n_q, const int32_t* n_k, const int32_t* prefix,
+                 const int64_t* spd_off, const int64_t* spd_ld, void* plan, size_t plan_bytes,
+                 gt_attn_pack_t* out) {
+  std::vector<Graph> graphs;
+  graphs.reserve(G);
+  gt_attn_pack_t info{};
+  int64_t dense = 0;
+  for (int32_t g = 0; g < G; ++g) {
+    const int32_t a = n_q[g], b = n_k[g];
+    if (a < 0 || b < 0) return GT_ERR_INVALID;
+    if (a > kMaxNodes || b > kMaxNodes) return GT_ERR_UNSUPPORTED;
+    if (prefix && prefix[g] < 0) return GT_ERR_INVALID;
+    const int64_t ld = spd_ld ? spd_ld[g] : b;
+    const int64_t off = spd_off ? spd_off[g] : dense;
+    if (ld < b || off < 0) return GT_ERR_INVALID;
+    if (ld > kMaxNodes) return GT_ERR_UNSUPPORTED;
+    dense += (int64_t)a * b;
+    if (a > 0 && b > 0) {
+      const int64_t last = (int64_t)(a - 1) * ld + b;
+      if (off > std::numeric_limits<int64_t>::max() - last) return GT_ERR_INVALID;
+      info.spd_bytes = std::max(info.spd_bytes, off + last);
+    }
+    graphs.push_back({(int32_t)info.total_q, a, (int32_t)info.total_k, b,
+                      prefix ? prefix[g] : std::numeric_limits<int32_t>::max(), (int32_t)ld, off});
+    info.total_q += a;
+    info.total_k += b;
+    if (info.total_q > std::numeric_limits<int32_t>::max() || info.total_k > std::numeric_limits<int32_t>::max())
+      return GT_ERR_UNSUPPORTED;
+  }
+  info.n_graphs = G;
+  info.H = H;
+  Plan plans[3];
+  const Stage stages[3] = {kForward, kDq, kDkdv};
+  for (int i = 0; i < 3; ++i) {
+    plans[i] = best_plan(graphs, H, stages[i]);
+    if (((int64_t)plans[i].jobs.size() + 8) * H > std::numeric_limits<int32_t>::max()) return GT_ERR_UNSUPPORTED;
+  }
+  auto lay_out = [&](uint8_t* buf) {
+    size_t at = 0;
+    for (int i = 0; i < 3; ++i) {
+      info.jobs[i] = (int32_t)plans[i].jobs.size();
+      info.job_off[i] = place(at, plans[i].jobs, buf);
+      info.group_off[i] = place(at, plans[i].groups, buf);
+    }
+    info.merges = (int32_t)plans[kForward].merges.size();
+    info.parts = plans[kForward].parts;
+    info.merge_off = place(at, plans[kForward].merges, buf);
+    info.plan_bytes = (int64_t)at;
+  };
+  lay_out(nullptr);
+  *out = info;
+  if (plan) {
+    if (plan_bytes < (size_t)info.plan_bytes) return GT_ERR_WORKSPACE;
+    std::memset(plan, 0, (size_t)info.plan_bytes);
+    lay_out(static_cast<uint8_t*>(plan));
+  }
+  return GT_OK;
+}
+
+}  // namespace
+}  // namespace gt
+
+extern "C" gt_status_t gt_attn_pack_plan(int32_t n_graphs, int32_t H, const int32_t* n_q, const int32_t* n_k,
+                                         const int32_t* prefix, const int64_t* spd_off, const int64_t* spd_ld,
+                                         void* plan, size_t plan_bytes, gt_attn_pack_t* info) {
+  if (n_graphs < 1 || H < 1 || H > 65535 || !n_q || !n_k || !info) return GT_ERR_INVALID;
+  try {
+    return gt::make(n_graphs, H, n_q, n_k, prefix, spd_off, spd_ld, plan, plan_bytes, info);
+  } catch (...) {     // out of host memory
+    return GT_ERR_WORKSPACE;
+  }
+}

@@ -1,0 +1,300 @@
+"""Packed batches of graphs of unlike sizes: attention with capped scores, a
+prefix mask and dropout of the probabilities (C ABI gt_attn_pack_*, whose
+header states the definitions).
+
+    pack = gt_attn_pack([37, 12, 405], H=8)                  # graphs of 37, 12 and 405 nodes
+    o, lse = gt_attn_pack_fwd(q, k, v, spd, table, pack, cap=30.0, dropout=GTDropout(0.1, seed, step))
+    dq, dk, dv, dtable = gt_attn_pack_bwd(q, k, v, spd, table, pack, o, lse, d_o, cap=30.0,
+                                          dropout=GTDropout(0.1, seed, step))
+    pack = gt_attn_pack([1, 1], H=8, n_k=[900, 4000])        # one new node against each graph's keys
+    pack = gt_attn_pack(sizes, H=8, prefix=[0] * len(sizes)) # causal; prefix[g] first keys are seen by all
+
+q, k, v [H, T, d] hold the graphs' rows one behind the other (T may be larger
+than their total: the rows behind it are left alone); any strides whose last is
+1 and whose others are multiples of 16 bytes, so a [T, H, d] tensor is passed as
+x.transpose(0, 1). spd holds the graphs' [n_q, n_k] uint8 distances one behind
+the other.
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+from typing import NamedTuple
+
+import numpy as np
+import torch
+
+from . import (_F, _I32, _I64, _P, _check, _dt, _need, _ptr, _qdims, _raw_stream, _shape, _table, _workspace, lib)
+
+__all__ = ["GTDropout", "GTPack", "gt_attn_pack", "gt_attn_pack_bwd", "gt_attn_pack_bwd_workspace_size",
+           "gt_attn_pack_fwd", "gt_attn_pack_fwd_workspace_size"]
+
+
+class GTDropout(NamedTuple):
+    """Dropout of the attention probabilities: rate p, 64-bit seed, and a 32-bit
+    offset (a layer and step number, say). offset_dev: an int32 device tensor of
+    one element that is added to offset when the kernels run, so that replays of
+    a captured graph can draw anew. The backward takes what the forward took."""
+    p: float
+    seed: int
+    offset: int = 0
+    offset_dev: torch.Tensor | None = None
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("p", _P), ("head_stride", _I64), ("row_stride", _I64)]
+
+
+class _Info(ctypes.Structure):
+    _fields_ = [("total_q", _I64), ("total_k", _I64), ("spd_bytes", _I64), ("plan_bytes", _I64),
+                ("n_graphs", _I32), ("H", _I32), ("jobs", _I32 * 3), ("merges", _I32), ("parts", _I32),
+                ("reserved", _I32), ("job_off", _I64 * 3), ("group_off", _I64 * 3), ("merge_off", _I64)]
+
+
+class _Dropout(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_double), ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint32), ("offset_dev", _P)]
+
+
+def _register(L: ctypes.CDLL) -> None:
+    R, Z = ctypes.POINTER(_Rows), ctypes.c_size_t
+    info, drop = ctypes.POINTER(_Info), ctypes.POINTER(_Dropout)
+    L.gt_attn_pack_plan.restype = _I32
+    L.gt_attn_pack_plan.argtypes = [_I32, _I32, _P, _P, _P, _P, _P, _P, Z, info]
+    L.gt_attn_pack_fwd_workspace_size.restype = Z
+    L.gt_attn_pack_fwd_workspace_size.argtypes = [info, _I32]
+    L.gt_attn_pack_bwd_workspace_size.restype = Z
+    L.gt_attn_pack_bwd_workspace_size.argtypes = [info, _I32]
+    L.gt_attn_pack_fwd.restype = _I32
+    L.gt_attn_pack_fwd.argtypes = [info, _P, R, R, R, _P, _P, _I32, R, _P, _I64, _P, Z, _I32, _I32, _F, _F, drop, _P]
+    L.gt_attn_pack_bwd.restype = _I32
+    L.gt_attn_pack_bwd.argtypes = [info, _P, R, R, R, _P, _P, _I32, R, _P, _I64, R, R, R, R, _P, _P, Z, _I32, _I32,
+                                   _F, _F, drop, _P]
+
+
+class GTPack:
+    """A packed batch's sizes and its plan on the device (from gt_attn_pack).
+    total_q, total_k: packed rows; spd_bytes: bytes of distances; H: heads."""
+
+    def __init__(self, info: _Info, plan: torch.Tensor):
+        self._info = info
+        self._plan = plan
+        self.total_q, self.total_k = info.total_q, info.total_k
+        self.spd_bytes, self.H, self.n_graphs = info.spd_bytes, info.H, info.n_graphs
+        self.device = plan.device
+
+
+def _sizes(x, name: str, n: int | None, dtype=np.int32) -> np.ndarray:
+    a = np.asarray(x)
+    _need(a.ndim == 1 and (a.size == 0 or a.dtype.kind in "iu"), f"{name} must be a sequence of whole numbers")
+    _need(n is None or a.size == n, f"{name} must have one entry per graph")
+    _need(a.size > 0, f"{name} must not be empty")
+    lim = np.iinfo(dtype).max
+    _need(int(a.min()) >= 0 and int(a.max()) <= lim, f"{name} must lie in 0..{lim}")
+    return np.ascontiguousarray(a, dtype=dtype)
+
+
+def gt_attn_pack(n_q, H: int, n_k=None, prefix=None, spd_off=None, spd_ld=None, device="cuda") -> GTPack:
+    """The plan of a packed batch (C ABI gt_attn_pack_plan) for graphs of n_q[g]
+    query rows and n_k[g] keys (n_q by default) and H heads. prefix: None, or the
+    number of leading keys that every row of a graph sees beside those up to its own
+    position (0: causal). spd_off, spd_ld: where a graph's distances lie in spd and
+    their row stride, where they are not dense, one matrix behind the other. Made
+    once per batch of sizes, it serves every layer's and step's calls."""
+    nq = _sizes(n_q, "n_q", None)
+    nk = nq if n_k is None else _sizes(n_k, "n_k", nq.size)
+    opt = [None if x is None else _sizes(x, name, nq.size, t)
+           for x, name, t in ((prefix, "prefix", np.int32), (spd_off, "spd_off", np.int64), (spd_ld, "spd_ld", np.int64))]
+    _need(isinstance(H, int) and 1 <= H <= 65535, "H must lie in 1..65535")
+    info = _Info()
+
+    def call(buf):
+        return lib().gt_attn_pack_plan(nq.size, H, nq.ctypes.data, nk.ctypes.data,
+                                       *(None if x is None else x.ctypes.data for x in opt),
+                                       None if buf is None else buf.ctypes.data,
+                                       0 if buf is None else buf.nbytes, ctypes.byref(info))
+
+    # (about 64 bytes per 32 rows and list in most plans; a second call where it is more)
+    blocks = int((nq.astype(np.int64) + 31).sum() + (nk.astype(np.int64) + 31).sum()) // 32
+    buf = np.empty(4096 + 256 * (blocks + nq.size), dtype=np.uint8)
+    st = call(buf)
+    if st == 3 and info.plan_bytes > buf.nbytes:
+        buf = np.empty(info.plan_bytes, dtype=np.uint8)
+        st = call(buf)
+    _check(st, "gt_attn_pack_plan")
+    return GTPack(info, torch.from_numpy(buf[:max(1, info.plan_bytes)]).to(device))
+
+
+def gt_attn_pack_fwd_workspace_size(pack: GTPack, d: int) -> int:
+    return int(lib().gt_attn_pack_fwd_workspace_size(ctypes.byref(pack._info), d))
+
+
+def gt_attn_pack_bwd_workspace_size(pack: GTPack, n_buckets: int) -> int:
+    return int(lib().gt_attn_pack_bwd_workspace_size(ctypes.byref(pack._info), n_buckets))
+
+
+def _rows(t, name: str, H: int, rows: int, d: int, dtype, written: bool = False) -> _Rows:
+    """A [H, >= rows, d] tensor as the C ABI's rows."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 3:
+        raise ValueError(f"{name} must be a 3-D tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    n = t.shape[1]
+    if t.shape[0] != H or t.shape[2] != d or n < rows:
+        raise ValueError(f"{name} must have shape ({H}, >= {rows}, {d}), got {tuple(t.shape)}")
+    hs, rs, one = t.stride()
+    unit = 8 if dtype == torch.bfloat16 else 4
+    if one != 1 or (rows > 1 and (rs % unit or not d <= rs <= 1 << 23)) or (H > 1 and (hs % unit or hs < 0)):
+        raise ValueError(f"{name} must have unit feature stride, and row and head strides that are multiples of 16 "
+                         f"bytes, the row stride in {d}..{1 << 23}; got {t.stride()}")
+    if t.data_ptr() % 16:
+        raise ValueError(f"{name} must be 16-byte aligned")
+    if written and H > 1 and rows > 0 and not (hs >= (rows - 1) * rs + d or rs >= (H - 1) * hs + d and hs >= d):
+        raise ValueError(f"{name} is written: its rows must not overlap")
+    # (a stride that no element is reached by may be anything in torch)
+    return _Rows(t.data_ptr(), hs if H > 1 else 0, rs if rows > 1 else max(d, unit))
+
+
+def _dropout(dropout, dev: int):
+    if dropout is None or dropout.p == 0:
+        return None
+    p, seed, offset, dyn = dropout
+    _need(0.0 <= p < 1.0 and round(p * 65536) <= 65535, f"dropout must lie in 0 <= p < 1 - 2^-17, got {p}")
+    _need(0 <= seed < 1 << 64, "seed must be a 64-bit unsigned number")
+    _need(0 <= offset < 1 << 32, "offset must be a 32-bit unsigned number")
+    if dyn is not None:
+        _need(isinstance(dyn, torch.Tensor) and dyn.dtype == torch.int32 and dyn.numel() == 1 and dyn.is_cuda
+              and dyn.get_device() == dev, "offset_dev must be an int32 tensor of one element on q's device")
+    return ctypes.byref(_Dropout(p, seed, offset, _ptr(dyn)))
+
+
+def _common(q, k, v, spd, table, pack, scale, cap):
+    """Checks of both calls; returns what they pass on."""
+    if not isinstance(pack, GTPack):
+        raise ValueError("pack must come from gt_attn_pack")
+    if isinstance(q, torch.Tensor) and q.dim() == 3 and q.shape[1] == 0:
+        dt = q.dtype                                   # a batch without query rows
+    else:
+        dt = _qdims(q, "q", 3)
+    H, _, d = q.shape
+    _need(H == pack.H, f"the plan is for {pack.H} heads, q has {H}")
+    rows = [_rows(q, "q", H, pack.total_q, d, dt), _rows(k, "k", H, pack.total_k, d, dt),
+            _rows(v, "v", H, pack.total_k, d, dt)]
+    _need(k.shape == v.shape, "k and v must have one shape")
+    if not (isinstance(spd, torch.Tensor) and spd.dtype == torch.uint8 and spd.is_contiguous()
+            and spd.numel() >= pack.spd_bytes):
+        raise ValueError(f"spd must be a contiguous uint8 tensor of at least {pack.spd_bytes} bytes")
+    _table(table, H)
+    _need(table.is_contiguous(), "table must be contiguous")
+    _need(q.is_cuda, "tensors must be device tensors")
+    dev = q.get_device()
+    _need(pack._plan.get_device() == dev, "the plan must be on q's device")
+    _same_device(dev, k, v, spd, table)
+    scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
+    cap = 0.0 if cap is None else float(cap)
+    _need(0.0 <= cap < math.inf, f"cap must be positive and finite, or None, got {cap}")
+    return dt, H, d, dev, rows, scale, cap
+
+
+def _same_device(dev: int, *ts):
+    for t in ts:
+        if t is not None and t.get_device() != dev:
+            raise ValueError("tensors must be device tensors on one device")
+
+
+def _lse(lse, H: int, T: int):
+    _need(isinstance(lse, torch.Tensor) and lse.dtype == torch.float32 and lse.shape == (H, T) and lse.is_contiguous(),
+          f"lse must be a contiguous float32 tensor of shape ({H}, {T})")
+
+
+def _on_stream(dev: int, stream, *held):
+    """The raw stream of a call (dev's current one by default). What the call
+    allocated on the current stream, and the plan, are kept from reuse until a
+    stream of the caller's choice has passed it."""
+    cur = torch.cuda.current_stream(dev) if stream is not None or _raw_stream is None else None
+    if stream is None:
+        return _raw_stream(dev) if cur is None else cur.cuda_stream
+    _need(stream.device_index == dev, "stream must be of the tensors' device")
+    if stream.cuda_stream != cur.cuda_stream:
+        for t in held:
+            if t is not None and t.numel():
+                t.record_stream(stream)
+    return stream.cuda_stream
+
+
+def _launch(dev: int, fn, *args) -> int:
+    # kernels are launched on the current device, which must be the tensors'
+    if torch.cuda.current_device() == dev:
+        return fn(*args)
+    with torch.cuda.device(dev):
+        return fn(*args)
+
+
+def gt_attn_pack_fwd(q, k, v, spd, table, pack: GTPack, scale: float | None = None, cap: float | None = None,
+                     dropout: GTDropout | None = None, out=None, lse=None, workspace=None, stream=None):
+    """O [H, T, d] (q's type) and LSE [H, T] fp32 of the packed batch (C ABI
+    gt_attn_pack_fwd). cap: bound of the scores before the bias, None for none;
+    dropout: GTDropout or None. Rows behind the batch's total stay as they are
+    (uninitialised where the call allocates)."""
+    dt, H, d, dev, (rq, rk, rv), scale, cap = _common(q, k, v, spd, table, pack, scale, cap)
+    T = q.shape[1]
+    drop = _dropout(dropout, dev)
+    made = []
+    if out is None:
+        out = torch.empty((H, T, d), device=q.device, dtype=dt)
+        made.append(out)
+    if lse is None:
+        lse = torch.empty((H, T), device=q.device, dtype=torch.float32)
+        made.append(lse)
+    ro = _rows(out, "out", H, pack.total_q, d, dt, written=True)
+    _lse(lse, H, T)
+    _same_device(dev, out, lse)
+    need = gt_attn_pack_fwd_workspace_size(pack, d)
+    if workspace is not None:
+        _workspace(workspace, need, q)
+    elif need:
+        workspace = torch.empty(need, device=q.device, dtype=torch.uint8)
+        made.append(workspace)
+    s = _on_stream(dev, stream, pack._plan, *made)
+    b = ctypes.byref
+    st = _launch(dev, lib().gt_attn_pack_fwd, b(pack._info), _ptr(pack._plan), b(rq), b(rk), b(rv), _ptr(spd),
+                 _ptr(table), table.shape[1], b(ro), _ptr(lse), T, _ptr(workspace),
+                 0 if workspace is None else workspace.numel(), d, _dt(q), scale, cap, drop, s)
+    _check(st, "gt_attn_pack_fwd")
+    return out, lse
+
+
+def gt_attn_pack_bwd(q, k, v, spd, table, pack: GTPack, o, lse, d_o, scale: float | None = None,
+                     cap: float | None = None, dropout: GTDropout | None = None, workspace=None, grads=None,
+                     stream=None):
+    """dQ, dK, dV and dTable of the packed batch (C ABI gt_attn_pack_bwd), with
+    the forward's arguments and results. `grads` may hold preallocated (dq, dk,
+    dv, dtable); rows behind the batch's totals stay as they are."""
+    dt, H, d, dev, (rq, rk, rv), scale, cap = _common(q, k, v, spd, table, pack, scale, cap)
+    T, nb = q.shape[1], table.shape[1]
+    drop = _dropout(dropout, dev)
+    ro, rdo = _rows(o, "o", H, pack.total_q, d, dt), _rows(d_o, "d_o", H, pack.total_q, d, dt)
+    _lse(lse, H, T)
+    made = []
+    if grads is None:
+        grads = made = [torch.empty(x.shape, device=q.device, dtype=x.dtype) for x in (q, k, v, table)]
+    _need(len(grads) == 4, "grads must be (dq, dk, dv, dtable)")
+    dq, dk, dv, dtable = grads
+    rdq = _rows(dq, "dq", H, pack.total_q, d, dt, written=True)
+    rdk = _rows(dk, "dk", H, pack.total_k, d, dt, written=True)
+    rdv = _rows(dv, "dv", H, pack.total_k, d, dt, written=True)
+    _shape(dtable, "dtable", table.shape, torch.float32)
+    _need(dtable.is_contiguous(), "dtable must be contiguous")
+    _same_device(dev, o, lse, d_o, dq, dk, dv, dtable)
+    need = gt_attn_pack_bwd_workspace_size(pack, nb)
+    if workspace is not None:
+        _workspace(workspace, need, q)
+    else:
+        workspace = torch.empty(need, device=q.device, dtype=torch.uint8)
+        made = [*made, workspace]
+    s = _on_stream(dev, stream, pack._plan, *made)
+    b = ctypes.byref
+    st = _launch(dev, lib().gt_attn_pack_bwd, b(pack._info), _ptr(pack._plan), b(rq), b(rk), b(rv), _ptr(spd),
+                 _ptr(table), nb, b(ro), _ptr(lse), T, b(rdo), b(rdq), b(rdk), b(rdv), _ptr(dtable),
+                 _ptr(workspace), workspace.numel(), d, _dt(q), scale, cap, drop, s)
+    _check(st, "gt_attn_pack_bwd")
+    return dq, dk, dv, dtable

@@ -1,0 +1,398 @@
+"""Packed attention (capped scores, prefix mask, dropout) against the fp64 oracle.
+
+Tolerances (2-norm of the error over that of the result), from the roundings on
+the way. A bf16 rounding is off by at most 2^-8 of the value:
+  bf16 O: P and O are rounded, 2 * 2^-8; dQ, dK, dV: O inside D, dU (or P), and
+  the result, 3 * 2^-8.
+  fp32 outputs of bf16 inputs (LSE, dtable): a capped score in base 2 is a sum of
+  terms of up to 2 cap log2 e <= 87 (cap 30), each off by half a step of 2^-24
+  relative, the reciprocal by 2^-23: P is off by at most 87 (2^-23 + 2^-24) ln 2 = 1.1e-5,
+  twice that for a difference from an LSE off as much: 2e-5.
+  fp32: 30 (2^-23 + 2^-24) = 5.4e-6 from the cap in P the same way, twice that and the sums: 2e-5.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import paper_2609_34420_amd as gt
+import synth
+from gpu_common import DEV, rel_l2, say, to_dev, to_np
+
+pytestmark = pytest.mark.gpu
+
+TOL = {"bf16": dict(o=2 * 2.0 ** -8, grad=3 * 2.0 ** -8, f32=2e-5), "f32": dict(o=2e-5, grad=2e-5, f32=2e-5)}
+
+
+def make(n_q, n_k, H, d, nb, dt, seed=0, gain=1.0, mask=0.0):
+    """Host arrays of a packed batch; mask: share of -inf table entries."""
+    g = np.random.default_rng(seed)
+    td = torch.bfloat16 if dt == "bf16" else torch.float32
+
+    def t(n, s):
+        x = (s * g.standard_normal((H, n, d))).astype(np.float32)
+        return synth.round_bf16(x) if dt == "bf16" else x
+
+    tq, tk = sum(n_q), sum(n_k)
+    a = dict(q=t(tq, gain), k=t(tk, gain), v=t(tk, 1), do=t(tq, 1), td=td,
+             table=(0.5 * g.standard_normal((H, nb))).astype(np.float32),
+             spd=g.integers(0, min(256, nb + 2), sum(x * y for x, y in zip(n_q, n_k))).astype(np.uint8))
+    if mask:
+        a["table"][g.random((H, nb)) < mask] = -np.inf
+    return a
+
+
+def upload(a):
+    r = {k: to_dev(a[k], a["td"]) for k in ("q", "k", "v", "do")}
+    r["spd"], r["table"] = to_dev(a["spd"], torch.uint8), to_dev(a["table"])
+    return r
+
+
+def compare(tag, dt, got, want, total=None):
+    names = ("O", "LSE", "dQ", "dK", "dV", "dtable")
+    for name, x, y in zip(names, got, want):
+        x = to_np(x)
+        assert np.array_equal(np.isneginf(x), np.isneginf(y)), (tag, name, "-inf rows")
+        fin = np.isfinite(y)
+        assert np.isfinite(x[fin]).all(), (tag, name, "non-finite")
+        e = rel_l2(x[fin], y[fin])
+        lim = TOL[dt]["f32" if name in ("LSE", "dtable") else ("o" if name == "O" else "grad")]
+        say(f"{tag}: {name} {e:.2e} (limit {lim:.1e})")
+        assert e <= lim, (tag, name, e)
+
+
+def check(tag, n_q, H, d, nb, dt, n_k=None, prefix=None, cap=None, drop=None, seed=0, gain=1.0, mask=0.0, bwd=True):
+    say(tag)
+    n_k = n_q if n_k is None else n_k
+    a = make(n_q, n_k, H, d, nb, dt, seed, gain, mask)
+    r = upload(a)
+    pack = gt.gt_attn_pack(n_q, H, n_k=n_k, prefix=prefix, device=DEV)
+    kw = dict(cap=cap, dropout=drop)
+    args = (r["q"], r["k"], r["v"], r["spd"], r["table"], pack)
+    o, lse = gt.gt_attn_pack_fwd(*args, **kw)
+    got = [o, lse]
+    scale = 1 / math.sqrt(d)
+    okw = dict(cap=cap or 0.0, prefix=prefix, dropout=drop and (drop.p, drop.seed, drop.offset))
+    want = list(oracle.packed_forward(a["q"], a["k"], a["v"], a["spd"], a["table"], scale, n_q, n_k, **okw))
+    if bwd:
+        got += gt.gt_attn_pack_bwd(*args, o, lse, r["do"], **kw)
+        want += oracle.packed_backward(a["q"], a["k"], a["v"], a["spd"], a["table"], scale, a["do"], n_q, n_k, **okw)
+    torch.cuda.synchronize()
+    compare(tag, dt, got, want)
+    return r, pack, got
+
+
+RAGGED = [1, 31, 0, 32, 33, 64, 65, 100, 7, 129, 200]
+DROP = gt.GTDropout(0.1, 0x0123456789abcdef, 0xfffffffe)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [8, 16, 32, 64])
+@pytest.mark.parametrize("cap,drop", [(None, None), (3.0, None), (None, DROP), (30.0, DROP)])
+def test_ragged_batch(dt, d, cap, drop):
+    check(f"ragged {dt} d={d} cap={cap} drop={drop is not None}", RAGGED, 2, d, 20, dt, cap=cap, drop=drop, gain=1.5)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("cap,drop", [(None, None), (5.0, gt.GTDropout(0.5, 3))])
+@pytest.mark.parametrize("prefix", ["causal", "some", "past"])
+def test_prefix_mask(dt, cap, drop, prefix):
+    p = {"causal": 0, "some": 40, "past": 1000}[prefix]
+    check(f"prefix {dt} {prefix} cap={cap}", RAGGED, 2, 32, 30, dt, prefix=[p] * len(RAGGED), cap=cap, drop=drop)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("prefix", [None, 0, 50])
+def test_more_keys_than_rows_and_the_other_way(dt, prefix):
+    n_q, n_k = [1, 3, 40, 0, 70, 5, 129], [300, 0, 100, 9, 33, 5, 2]
+    check(f"rectangles {dt} prefix={prefix}", n_q, 3, 64, 40, dt, n_k=n_k, cap=10.0, drop=DROP,
+          prefix=None if prefix is None else [prefix] * len(n_q))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [16, 64])
+@pytest.mark.parametrize("n", [1, 2, 33])
+def test_new_rows_against_a_long_cache(dt, d, n):
+    """Few rows, keys split over workgroups and merged."""
+    n_q, n_k = [n, n], [6000, 2345]
+    _, pack, _ = check(f"cache {dt} d={d} n={n}", n_q, 2, d, 64, dt, n_k=n_k, cap=30.0, drop=DROP, bwd=n == 2)
+    assert pack._info.parts > 0
+    check(f"cache causal {dt} d={d} n={n}", n_q, 2, d, 64, dt, n_k=n_k, prefix=[0, 100], bwd=n == 2)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [300, 1000])
+@pytest.mark.parametrize("H", [1, 40])
+def test_split_and_unsplit_grids(dt, N, H):
+    """Columns shared by 4, 2 or 1 groups of waves."""
+    check(f"one graph {dt} N={N} H={H}", [N], H, 32, 22, dt, cap=20.0, drop=DROP)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("nb", [1, 2, 127, 128, 256])
+def test_bucket_counts(dt, nb):
+    check(f"buckets {dt} nb={nb}", [150, 40], 2, 16, nb, dt, cap=8.0)
+
+
+def test_many_small_graphs():
+    g = np.random.default_rng(5)
+    check("many small", [int(x) for x in g.integers(1, 50, 300)], 4, 8, 22, "bf16", cap=20.0, drop=DROP)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_masked_entries_and_empty_rows(dt):
+    """Table masks (-inf, and the type's lowest value, which counts as one),
+    with rows that they leave nothing."""
+    n = [70, 40]
+    a = make(n, n, 2, 32, 10, dt, seed=4)
+    a["table"][:, 3], a["table"][:, 4], a["table"][:, 5] = -np.inf, np.finfo(np.float32).min, -1e30
+    for base, w in ((0, 70), (70 * 70, 40)):
+        a["spd"][base + 7 * w:base + 8 * w] = 3 + np.arange(w) % 3        # row 7 of each graph
+    r = upload(a)
+    pack = gt.gt_attn_pack(n, 2, device=DEV)
+    args = (r["q"], r["k"], r["v"], r["spd"], r["table"], pack)
+    for cap in (None, 4.0):
+        o, lse = gt.gt_attn_pack_fwd(*args, cap=cap)
+        grads = gt.gt_attn_pack_bwd(*args, o, lse, r["do"], cap=cap)
+        torch.cuda.synchronize()
+        okw = dict(cap=cap or 0.0)
+        s = 1 / math.sqrt(32)
+        want = (*oracle.packed_forward(a["q"], a["k"], a["v"], a["spd"], a["table"], s, n, n, **okw),
+                *oracle.packed_backward(a["q"], a["k"], a["v"], a["spd"], a["table"], s, a["do"], n, n, **okw))
+        compare(f"masks {dt} cap={cap}", dt, (o, lse, *grads), want)
+        for row in (7, 77):
+            assert bool((o[:, row] == 0).all()) and bool(torch.isneginf(lse[:, row]).all())
+            assert bool((grads[0][:, row] == 0).all())
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_large_scores(dt):
+    """Scores of some thousands, capped and not: no overflow, and saturated tanh."""
+    n = [90]
+    a = make(n, n, 2, 32, 8, dt, seed=9, gain=30.0)
+    r = upload(a)
+    pack = gt.gt_attn_pack(n, 2, device=DEV)
+    args = (r["q"], r["k"], r["v"], r["spd"], r["table"], pack)
+    for cap in (30.0, None):
+        o, lse = gt.gt_attn_pack_fwd(*args, cap=cap)
+        grads = gt.gt_attn_pack_bwd(*args, o, lse, r["do"], cap=cap)
+        torch.cuda.synchronize()
+        want = oracle.packed_forward(a["q"], a["k"], a["v"], a["spd"], a["table"], 32 ** -0.5, n, n, cap=cap or 0.0)
+        # uncapped scores of up to 2e4 are off by up to 2^-24 of that: P by 2e-3
+        e = rel_l2(to_np(o), want[0])
+        say(f"large {dt} cap={cap}: O {e:.2e}")
+        assert e <= (TOL[dt]["o"] if cap else TOL[dt]["o"] + 3e-3)
+        assert all(bool(torch.isfinite(x.float()).all()) for x in grads)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_nonfinite_values_stay_in_their_graph(bad):
+    n, H = [20, 40, 9, 100, 33, 64], 2
+    a = make(n, n, H, 32, 12, "bf16", seed=2)
+    ref = upload(a)
+    pack = gt.gt_attn_pack(n, H, device=DEV)
+
+    def run(r):
+        args = (r["q"], r["k"], r["v"], r["spd"], r["table"], pack)
+        o, lse = gt.gt_attn_pack_fwd(*args, cap=9.0, dropout=DROP)
+        return o, lse, *gt.gt_attn_pack_bwd(*args, ref_o[0], ref_o[1], r["do"], cap=9.0, dropout=DROP)
+
+    ref_o = gt.gt_attn_pack_fwd(ref["q"], ref["k"], ref["v"], ref["spd"], ref["table"], pack, cap=9.0, dropout=DROP)
+    want = run(ref)
+    for name in ("q", "k", "v", "do"):
+        r = dict(ref)
+        r[name] = ref[name].clone()
+        r[name][:, 25, 3] = bad                        # in the second graph, rows 20 .. 59
+        got = run(r)
+        torch.cuda.synchronize()
+        for x, y in zip(got[:5], want[:5]):
+            assert torch.equal(x[:, :20], y[:, :20]) and torch.equal(x[:, 60:], y[:, 60:]), name
+        # (an infinite K gives scores of +-inf, which the cap makes +-cap: finite)
+        if name == "v" or (name == "k" and math.isnan(bad)):
+            assert not bool(torch.isfinite(got[0][:, 20:60].float()).all())
+            assert bool(torch.isnan(got[5]).all())
+
+
+def test_rows_behind_the_batch_and_layouts():
+    """T beyond the batch's total: nothing there is read or written. Row-major
+    [T, H, d] storage, K shared by the heads, padded distances."""
+    n, H, d, T = [50, 21], 2, 32, 90
+    a = make(n, n, H, d, 12, "bf16", seed=3)
+    r = upload(a)
+    pack = gt.gt_attn_pack(n, H, device=DEV)
+    want = gt.gt_attn_pack_fwd(r["q"], r["k"], r["v"], r["spd"], r["table"], pack, cap=5.0)
+    gw = gt.gt_attn_pack_bwd(r["q"], r["k"], r["v"], r["spd"], r["table"], pack, *want, r["do"], cap=5.0)
+    nan = float("nan")
+
+    def wide(x, layout):
+        shape = (H, T, d) if layout == "htd" else (T, H, d)
+        y = torch.full(shape, nan, device=DEV, dtype=x.dtype)
+        y = y if layout == "htd" else y.transpose(0, 1)
+        y[:, :x.shape[1]] = x
+        return y
+
+    # the same distances with row strides 64 and 33, the second graph's first
+    ld, off = [64, 33], [33 * 21 + 5, 3]
+    spd = torch.full((off[0] + 64 * 50,), 255, dtype=torch.uint8, device=DEV)
+    for g, (s0, w) in enumerate(((0, 50), (2500, 21))):
+        for i in range(w):
+            spd[off[g] + i * ld[g]:off[g] + i * ld[g] + w] = r["spd"][s0 + i * w:s0 + (i + 1) * w]
+    pack2 = gt.gt_attn_pack(n, H, spd_off=off, spd_ld=ld, device=DEV)
+    for layout in ("htd", "thd"):
+        x = {k: wide(r[k], layout) for k in ("q", "k", "v", "do")}
+        out = wide(torch.zeros(H, 0, d, device=DEV, dtype=torch.bfloat16), layout)
+        lse = torch.full((H, T), nan, device=DEV)
+        gt.gt_attn_pack_fwd(x["q"], x["k"], x["v"], spd, r["table"], pack2, cap=5.0, out=out, lse=lse)
+        grads = [wide(torch.zeros(H, 0, d, device=DEV, dtype=torch.bfloat16), layout) for _ in range(3)]
+        grads.append(torch.empty_like(r["table"]))
+        gt.gt_attn_pack_bwd(x["q"], x["k"], x["v"], spd, r["table"], pack2, out, lse, x["do"], cap=5.0, grads=grads)
+        torch.cuda.synchronize()
+        for y, w in zip((out, lse, *grads[:3]), (*want, *gw[:3])):
+            assert torch.equal(y[:, :71], w) and bool(torch.isnan(y[:, 71:]).all()), layout
+        assert torch.equal(grads[3], gw[3])
+    shared = r["k"][:1].expand(H, -1, -1)
+    got = gt.gt_attn_pack_fwd(r["q"], shared, r["v"], r["spd"], r["table"], pack)
+    ref = gt.gt_attn_pack_fwd(r["q"], shared.contiguous(), r["v"], r["spd"], r["table"], pack)
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
+
+
+def test_empty_batches():
+    H, d = 2, 16
+    t = torch.zeros(H, 3, device=DEV)
+    e = torch.zeros(H, 0, d, device=DEV, dtype=torch.bfloat16)
+    spd = torch.zeros(0, dtype=torch.uint8, device=DEV)
+    pack = gt.gt_attn_pack([0, 0], H, device=DEV)
+    o, lse = gt.gt_attn_pack_fwd(e, e, e, spd, t, pack)
+    g = gt.gt_attn_pack_bwd(e, e, e, spd, t, pack, o, lse, e)
+    torch.cuda.synchronize()
+    assert o.shape == (H, 0, d) and bool((g[3] == 0).all())
+    x = torch.ones(H, 40, d, device=DEV, dtype=torch.bfloat16)
+    pack = gt.gt_attn_pack([40, 0], H, n_k=[0, 40], device=DEV)      # rows without keys, keys without rows
+    o, lse = gt.gt_attn_pack_fwd(x, x, x, spd, t, pack, cap=3.0)
+    g = gt.gt_attn_pack_bwd(x, x, x, spd, t, pack, o, lse, x, cap=3.0)
+    torch.cuda.synchronize()
+    assert bool((o == 0).all()) and bool(torch.isneginf(lse).all())
+    assert all(bool((y == 0).all()) for y in g)
+
+
+def test_bitwise_reproducible():
+    n = [700, 90, 33, 1200]
+    a = make(n, n, 4, 64, 40, "bf16", seed=6)
+    r = upload(a)
+    pack = gt.gt_attn_pack(n, 4, device=DEV)
+    args = (r["q"], r["k"], r["v"], r["spd"], r["table"], pack)
+
+    def run():
+        o, lse = gt.gt_attn_pack_fwd(*args, cap=20.0, dropout=DROP)
+        return o, lse, *gt.gt_attn_pack_bwd(*args, o, lse, r["do"], cap=20.0, dropout=DROP)
+
+    want = run()
+    for _ in range(3):
+        assert all(torch.equal(x, y) for x, y in zip(run(), want))
+
+
+def test_dropout_is_the_generators():
+    """V of unit vectors shows each kept pair; its share and place are the
+    oracle's; another offset gives another mask, offset_dev adds to offset."""
+    n, H, d, p = 64, 2, 64, 0.3
+    q = torch.zeros(H, n, d, device=DEV)
+    v = torch.eye(n, device=DEV).expand(H, n, n).contiguous()
+    t, spd = torch.zeros(H, 1, device=DEV), torch.zeros(n * n, dtype=torch.uint8, device=DEV)
+    pack = gt.gt_attn_pack([n], H, device=DEV)
+
+    def mask(**kw):
+        return gt.gt_attn_pack_fwd(q, q, v, spd, t, pack, dropout=gt.GTDropout(p, 99, **kw))[0] > 0
+
+    got = mask(offset=5)
+    for h in range(H):
+        assert np.array_equal(got[h].cpu().numpy(), oracle.keep_mask(range(n), n, h, p, 99, 5) > 0)
+    assert not torch.equal(got, mask(offset=6))
+    dyn = torch.tensor([-1], dtype=torch.int32, device=DEV)
+    assert torch.equal(got, mask(offset=6, offset_dev=dyn))
+
+
+def test_captured_steps_draw_anew():
+    """A training step captured into a graph and replayed, with eager work and
+    synchronisation between the replays; the offset moves on the device."""
+    n, H = [300, 45], 4
+    a = make(n, n, H, 32, 22, "bf16", seed=8)
+    r = upload(a)
+    pack = gt.gt_attn_pack(n, H, device=DEV)
+    dyn = torch.zeros(1, dtype=torch.int32, device=DEV)
+    args = (r["q"], r["k"], r["v"], r["spd"], r["table"], pack)
+
+    def step(drop):
+        o, lse = gt.gt_attn_pack_fwd(*args, cap=20.0, dropout=drop)
+        return o, lse, *gt.gt_attn_pack_bwd(*args, o, lse, r["do"], cap=20.0, dropout=drop)
+
+    drop = gt.GTDropout(0.2, 7, 100, dyn)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(drop)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(drop)
+        dyn.add_(1)
+    dyn.zero_()
+    for k in range(4):
+        graph.replay()
+        torch.cuda.synchronize()
+        want = step(gt.GTDropout(0.2, 7, 100 + k))
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, want)), k
+
+
+def test_streams_and_workspaces():
+    """Two streams at once with workspaces of the caller's and of the call's own."""
+    n, H = [400, 100], 4
+    runs = []
+    for seed in (1, 2):
+        r = upload(make(n, n, H, 32, 22, "bf16", seed=seed))
+        pack = gt.gt_attn_pack(n, H, device=DEV)
+        args = (r["q"], r["k"], r["v"], r["spd"], r["table"], pack)
+        o, lse = gt.gt_attn_pack_fwd(*args, dropout=DROP)
+        runs.append((args, r["do"], (o, lse, *gt.gt_attn_pack_bwd(*args, o, lse, r["do"], dropout=DROP))))
+    torch.cuda.synchronize()
+    need = gt.gt_attn_pack_bwd_workspace_size(runs[0][0][5], 22)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    ws = [None, torch.empty(need, dtype=torch.uint8, device=DEV)]
+    for _ in range(3):
+        got = []
+        for (args, do, _), s, w in zip(runs, streams, ws):
+            o, lse = gt.gt_attn_pack_fwd(*args, dropout=DROP, stream=s)
+            got.append((o, lse, *gt.gt_attn_pack_bwd(*args, o, lse, do, dropout=DROP, workspace=w, stream=s)))
+        torch.cuda.synchronize()
+        for (_, _, want), g in zip(runs, got):
+            assert all(torch.equal(x, y) for x, y in zip(g, want))
+    with pytest.raises(ValueError, match="workspace"):
+        gt.gt_attn_pack_bwd(*runs[0][0], *runs[0][2][:2], runs[0][1], workspace=ws[1][:need - 1])
+
+
+def test_agrees_with_the_unpacked_calls():
+    """No option on: the packed call is the framework's attention of each graph."""
+    n, H, d = [256, 77, 500], 2, 32
+    a = make(n, n, H, d, 22, "bf16", seed=11)
+    r = upload(a)
+    pack = gt.gt_attn_pack(n, H, device=DEV)
+    o, lse = gt.gt_attn_pack_fwd(r["q"], r["k"], r["v"], r["spd"], r["table"], pack)
+    grads = gt.gt_attn_pack_bwd(r["q"], r["k"], r["v"], r["spd"], r["table"], pack, o, lse, r["do"])
+    s0 = t0 = 0
+    dt = torch.zeros_like(r["table"])
+    for w in n:
+        x = [r[k][:, t0:t0 + w].contiguous() for k in ("q", "k", "v", "do")]
+        m = r["spd"][s0:s0 + w * w].view(w, w).clone()
+        oo, ll = gt.gt_attn_fwd(*x[:3], m, r["table"])
+        gg = gt.gt_attn_bwd(*x[:3], m, r["table"], oo, ll, x[3])
+        # two results, each off by the bf16 tolerances
+        for y, z, tol in zip((o, *grads[:3]), (oo, *gg[:3]), (2, 3, 3, 3)):
+            assert rel_l2(to_np(y[:, t0:t0 + w]), to_np(z)) <= 2 * tol * 2.0 ** -8
+        dt += gg[3]
+        s0, t0 = s0 + w * w, t0 + w
+    # the unpacked table gradient takes D from the rounded O
+    assert rel_l2(to_np(grads[3]), to_np(dt)) <= 1e-2
