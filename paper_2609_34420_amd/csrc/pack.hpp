@@ -14,8 +14,8 @@
 // takes them (perm32). Two policies give the products and the staging: Bf16Pack
 // (v_mfma_f32_32x32x16_bf16) and F32Pack (v_mfma_f32_32x32x2_f32).
 //
-// Two workgroups of 4 waves per compute unit, each with one staged tile; the
-// next tile's rows are in flight in registers meanwhile.
+// Tiles of bf16 rows go straight to LDS, tiles of fp32 rows, whose LDS rows are
+// padded, through registers.
 #pragma once
 #include <type_traits>
 
@@ -62,8 +62,20 @@ struct PackArgs {
 
 namespace {
 
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+
 constexpr int kPackThreads = kPackWaves * 64;
 constexpr float kNoScore = -1e30f;        // table entries at or below it are masks, as -inf
+
+// Wave-uniform values that the compiler took for divergent (a buffer resource of
+// such is read lane by lane).
+__device__ __forceinline__ bool uniform(bool x) { return __builtin_amdgcn_readfirstlane((int)x) != 0; }
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ const uint8_t* uniform(const uint8_t* p) {
+  const uint64_t x = reinterpret_cast<uint64_t>(p);
+  return reinterpret_cast<const uint8_t*>((uint64_t)(uint32_t)uniform((int)(uint32_t)x) |
+                                          (uint64_t)(uint32_t)uniform((int)(uint32_t)(x >> 32)) << 32);
+}
 
 // ---------------------------------------------------------------------------
 // Philox4x32 with 7 rounds (Salmon et al., Parallel random numbers: as easy as
@@ -72,40 +84,117 @@ constexpr float kNoScore = -1e30f;        // table entries at or below it are ma
 // draw gives the 8 keys of a row from a multiple of 8 on 16 bits each, key 2 w
 // in the low half of word w. 16 bits place p within 2^-17, and the kept pairs
 // are scaled by the exact inverse of the rate so placed.
+//
+// A 64-bit product costs some eight simple instructions, and a draw has 14. The
+// counter's words meet only after two rounds: up to then each product goes by
+// the row alone, or the keys alone, or neither. RowDraw and KeyDraw hold what the
+// products of one side leave, made once per row and once per 8 keys; 9 products
+// remain for the pair.
 // ---------------------------------------------------------------------------
-__device__ __forceinline__ uint4 philox7(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0, uint32_t k1) {
-#pragma unroll
-  for (int i = 0; i < 7; ++i) {
-    const uint64_t x = (uint64_t)c0 * 0xD2511F53u, y = (uint64_t)c2 * 0xCD9E8D57u;
-    c0 = (uint32_t)(y >> 32) ^ c1 ^ k0;
-    c2 = (uint32_t)(x >> 32) ^ c3 ^ k1;
-    c1 = (uint32_t)y;
-    c3 = (uint32_t)x;
-    k0 += 0x9E3779B9u;
-    k1 += 0xBB67AE85u;
-  }
-  return make_uint4(c0, c1, c2, c3);
+constexpr uint32_t kPhiloxM0 = 0xD2511F53u, kPhiloxM1 = 0xCD9E8D57u;
+constexpr uint32_t kPhiloxW0 = 0x9E3779B9u, kPhiloxW1 = 0xBB67AE85u;
+__device__ __forceinline__ uint32_t mul_hi_lo(uint32_t x, uint32_t m, uint32_t& lo) {
+  const uint64_t y = (uint64_t)x * m;
+  lo = (uint32_t)y;
+  return (uint32_t)(y >> 32);
 }
 
-// The random halves of 16 consecutive keys of packed row `row` from key j (a
-// multiple of 16) on: word w holds keys j + 2 w (low) and j + 2 w + 1.
-__device__ __forceinline__ void draw16(const PackArgs& a, uint32_t offset, int h, uint32_t row, int j, uint32_t (&w)[8]) {
-  const uint4 x = philox7((uint32_t)(j >> 3), row, (uint32_t)h, offset, a.seed0, a.seed1);
-  const uint4 y = philox7((uint32_t)(j >> 3) + 1u, row, (uint32_t)h, offset, a.seed0, a.seed1);
-  w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
-  w[4] = y.x; w[5] = y.y; w[6] = y.z; w[7] = y.w;
-}
+struct RowDraw { uint32_t xh, xl; };             // second round's product of the row's word
+struct Philox {
+  uint32_t k0, k1, offset;                       // (wave-uniform)
+  uint32_t hh, hl;                               // first round's product of the head's word
+  __device__ __forceinline__ Philox(const PackArgs& a, int h)
+      : k0(a.seed0), k1(a.seed1), offset(a.offset + (a.offset_dev ? *a.offset_dev : 0u)) {
+    hh = mul_hi_lo((uint32_t)h, kPhiloxM1, hl);
+  }
+  __device__ __forceinline__ RowDraw row(uint32_t packed_row) const {
+    RowDraw r;
+    r.xh = mul_hi_lo(hh ^ packed_row ^ k0, kPhiloxM0, r.xl);
+    return r;
+  }
+  // Keys 8 j8 .. + 7: what the third round takes of the first two, and its own
+  // product of the first word.
+  __device__ __forceinline__ uint4 keys(uint32_t j8) const {
+    uint4 k;
+    uint32_t x1, y2, x3;
+    const uint32_t c2 = mul_hi_lo(j8, kPhiloxM0, x1) ^ offset ^ k1;
+    const uint32_t c0 = mul_hi_lo(c2, kPhiloxM1, y2) ^ hl ^ (k0 + kPhiloxW0);
+    k.z = mul_hi_lo(c0, kPhiloxM0, x3) ^ (k1 + 2u * kPhiloxW1);
+    k.x = x1 ^ (k1 + kPhiloxW1);
+    k.y = y2 ^ (k0 + 2u * kPhiloxW0);
+    k.w = x3;
+    return k;
+  }
+  __device__ __forceinline__ void draw(const RowDraw& r, const uint4& k, uint32_t* w) const {
+    uint32_t c1, c0 = mul_hi_lo(r.xh ^ k.x, kPhiloxM1, c1) ^ k.y, c2 = r.xl ^ k.z, c3 = k.w;
+#pragma unroll
+    for (uint32_t i = 3; i < 7; ++i) {
+      uint32_t x, y;
+      const uint32_t n0 = mul_hi_lo(c2, kPhiloxM1, y) ^ c1 ^ (k0 + i * kPhiloxW0);
+      c2 = mul_hi_lo(c0, kPhiloxM0, x) ^ c3 ^ (k1 + i * kPhiloxW1);
+      c0 = n0;
+      c1 = y;
+      c3 = x;
+    }
+    w[0] = c0; w[1] = c1; w[2] = c2; w[3] = c3;
+  }
+};
+// Pair r of 16 (two draws).
 __device__ __forceinline__ bool kept(const uint32_t (&w)[8], int r, int thr) {
   return (int)(int16_t)(w[r >> 1] >> (16 * (r & 1))) >= thr;
+}
+// The same of a word's two pairs: all ones in the halves of the kept ones (the
+// saturating difference keeps its sign; below: thr - 1 in both halves).
+__device__ __forceinline__ uint32_t kept2(uint32_t w, uint32_t below) {
+  const s16x2 d = __builtin_elementwise_sub_sat(__builtin_bit_cast(s16x2, below), __builtin_bit_cast(s16x2, w));
+  return __builtin_bit_cast(uint32_t, (s16x2)(d >> (short)15));
 }
 
 // ---------------------------------------------------------------------------
 // Scores. Units: bf16 works in base 2 (x = S log2 e), fp32 in S itself.
 // ---------------------------------------------------------------------------
 struct ScoreConst {
-  float mul, add;           // bf16, capped: e = 2^(s mul) = e^(2 u / cap), x = add / (e + 1) + bias
+  float mul;                // bf16: uncapped score = s mul; capped: e^(2 u / cap) = 2^(s mul)
+  float add;                // bf16, capped: score = cap log2 e - add / (e^(2 u / cap) + 1)
   float cap;                // fp32
 };
+
+// Capped scores are bounded, and with them, table and all, the exponents: where
+// they span at most kSpan, the softmax needs no running reference but takes one for
+// the whole head, `ref`, kBelow below their top, which the table's entries carry:
+// no addition per score, no test per block, and no rescaling. exp stays within
+// 2^-110 .. 2^70, so sums of 2^25 keys and values up to 2^32 stay finite, and nothing
+// of a row whose scores are all at the low end underflows. (A cap of 50 spans 144;
+// 36 are left for the biases.)
+constexpr float kSpan = 180.0f, kBelow = 70.0f;
+struct ScoreRef {
+  bool fixed;
+  float ref;
+};
+// From the workgroup's 256 entries (thread b: entry b, bias log2 e; 0 past the table).
+__device__ __forceinline__ ScoreRef score_ref(float entry, float cap2, float* lds) {
+  const bool mask = entry == -INFINITY;
+  float hi = mask ? -INFINITY : entry, lo = mask ? INFINITY : entry;
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) {
+    hi = fmaxf(hi, __shfl_xor(hi, o));
+    lo = fminf(lo, __shfl_xor(lo, o));
+  }
+  if ((threadIdx.x & 63) == 0) {
+    lds[2 * wave_id()] = hi;
+    lds[2 * wave_id() + 1] = lo;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kPackWaves; ++w) {
+    hi = fmaxf(hi, lds[2 * w]);
+    lo = fminf(lo, lds[2 * w + 1]);
+  }
+  ScoreRef r;
+  r.fixed = uniform(hi - lo + 2.0f * cap2 <= kSpan);   // (false for a NaN or infinite entry)
+  r.ref = r.fixed ? hi + cap2 - kBelow : 0.0f;
+  return r;
+}
 
 // D: the tile's head dim (32 or 64); DS <= D: the tensors'.
 template <int D_, int DS_>
@@ -121,12 +210,18 @@ struct Bf16Pack {
 
   __device__ __forceinline__ static int lds_off(int row, int ch) { return row * D + swz_tile<D>(row, ch) * 8; }
 
-  // The lane's stationary row (features past DS zero).
-  __device__ __forceinline__ static void load_operand(const T* row, bool ok, float, Operand& x) {
+  // The lane's stationary row (features past DS zero), times a power of two.
+  __device__ __forceinline__ static void load_operand(const T* row, bool ok, float mul, Operand& x) {
     const int g = (threadIdx.x >> 5) & 1;
 #pragma unroll
     for (int kc = 0; kc < D / 16; ++kc)
       x.f[kc] = ok && kc * 16 + g * 8 < DS ? *reinterpret_cast<const bf16x8*>(row + kc * 16 + g * 8) : zero_bf16x8();
+    if (mul != 1.0f) {
+#pragma unroll
+      for (int kc = 0; kc < D / 16; ++kc)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x.f[kc][e] = (__bf16)((float)x.f[kc][e] * mul);
+    }
   }
   // Dot product of two operands' features in this lane half.
   __device__ __forceinline__ static float dot(const Operand& x, const Operand& y) {
@@ -152,6 +247,28 @@ struct Bf16Pack {
   __device__ __forceinline__ static void cols(const T* tile, const float (&p)[16], f32x16 (&acc)[NA]) {
     cols(tile, cvt_bf16x8(p), cvt_bf16x8(p + 8), acc);
   }
+  // Two products of one tile.
+  __device__ __forceinline__ static void cols2(const T* tile, const float (&p)[16], f32x16 (&acc)[NA],
+                                               const float (&q)[16], f32x16 (&acc2)[NA]) {
+    const bf16x8 p0 = cvt_bf16x8(p), p1 = cvt_bf16x8(p + 8), q0 = cvt_bf16x8(q), q1 = cvt_bf16x8(q + 8);
+#pragma unroll
+    for (int cb = 0; cb < NA; ++cb) {
+      const int o0 = tr_operand_off<D>(0, cb), o1 = tr_operand_off<D>(1, cb);
+      const bf16x8 t0 = lds_tr_operand(tile, o0, o1), t1 = lds_tr_operand(tile + 8 * D, o0, o1);
+      acc[cb] = mfma32(t0, p0, acc[cb]);
+      acc2[cb] = mfma32(t0, q0, acc2[cb]);
+      acc[cb] = mfma32(t1, p1, acc[cb]);
+      acc2[cb] = mfma32(t1, q1, acc2[cb]);
+    }
+  }
+  // Both of p's products' bf16 operand with the dropped pairs (16 draws' bits) zero.
+  __device__ __forceinline__ static void cols_kept(const T* tile, const float (&p)[16], const uint32_t (&w)[8],
+                                                   uint32_t below, int, f32x16 (&acc)[NA]) {
+    uint4 x = __builtin_bit_cast(uint4, cvt_bf16x8(p)), y = __builtin_bit_cast(uint4, cvt_bf16x8(p + 8));
+    x.x &= kept2(w[0], below); x.y &= kept2(w[1], below); x.z &= kept2(w[2], below); x.w &= kept2(w[3], below);
+    y.x &= kept2(w[4], below); y.y &= kept2(w[5], below); y.z &= kept2(w[6], below); y.w &= kept2(w[7], below);
+    cols(tile, __builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), acc);
+  }
   // put(feature, 4 values) for the lane's column.
   template <typename F>
   __device__ __forceinline__ static void features(const f32x16 (&acc)[NA], F put) {
@@ -173,27 +290,35 @@ struct Bf16Pack {
 
   __device__ __forceinline__ static float operand_mul(const PackArgs&, bool) { return 1.0f; }
   __device__ __forceinline__ static ScoreConst consts(const PackArgs& a, bool cap) {
-    ScoreConst c;
+    ScoreConst c{};
     c.mul = a.scale * kLog2e * (cap ? 2.0f / a.cap : 1.0f);
-    c.add = -2.0f * a.cap * kLog2e;
-    c.cap = a.cap;
+    c.add = 2.0f * a.cap * kLog2e;
     return c;
   }
-  // Table entry in LDS: bias log2 e, and with a cap its log2 e too, since
-  // cap tanh(u / cap) = cap - 2 cap / (e^(2 u / cap) + 1).
-  __device__ __forceinline__ static float entry(float bias, const PackArgs& a, bool cap) {
-    return bias <= kNoScore ? -INFINITY : bias * kLog2e + (cap ? a.cap * kLog2e : 0.0f);
+  // Table entry in LDS: bias log2 e, or, as the start of the score accumulator,
+  // bias / scale.
+  __device__ __forceinline__ static float entry(float bias, const PackArgs& a, bool start) {
+    return bias <= kNoScore ? -INFINITY : (start ? bias / a.scale : bias * kLog2e);
   }
-  // Score from the product s; slope: dc/du (times 1/4 with a cap, see kSlope).
-  static constexpr float kSlope = 4.0f;
-  template <bool CAP>
-  __device__ __forceinline__ static float score(float s, float bias, const ScoreConst& c, float& slope) {
-    if constexpr (!CAP) return fmaf(s, c.mul, bias);
-    const float r = __builtin_amdgcn_rcpf(exp2_fast(s * c.mul) + 1.0f);
-    slope = fmaf(-r, r, r);                          // 1 - tanh^2 = 4 (r - r^2)
-    return fmaf(r, c.add, bias);
+  // x = S log2 e from the products s and the entries in x (which hold the cap's
+  // log2 e too, cap tanh(u / cap) = cap - 2 cap / (e^(2 u / cap) + 1); uncapped: s holds
+  // them already). SLOPE: slope = -dc/du / 4. (The exponential and the reciprocal run
+  // at half rate: a polynomial for scores below 3/4 of the cap, 7 instructions, was
+  // no faster.)
+  template <bool CAP, bool SLOPE>
+  __device__ __forceinline__ static void scores(const f32x16& s, float (&x)[16], float (&slope)[16],
+                                                const ScoreConst& c) {
+    static_assert(CAP, "uncapped scores come out of the product");
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float e = __builtin_amdgcn_rcpf(-1.0f - exp2_fast(s[r] * c.mul));
+      if constexpr (SLOPE) slope[r] = fmaf(e, e, e);               // 1 - tanh^2 = -4 (e^2 + e)
+      x[r] = fmaf(e, c.add, x[r]);
+    }
   }
-  __device__ __forceinline__ static float expo(float x, float mneg) { return exp2_fast(x + mneg); }
+  // What the sums of slope times anything are multiplied by.
+  static constexpr float kSlope = -4.0f;
+  __device__ __forceinline__ static float expo(float x) { return exp2_fast(x); }
   __device__ __forceinline__ static float to_unit(float lse) { return lse * kLog2e; }
   __device__ __forceinline__ static float log_sum(float m, float l) { return (m + __log2f(l)) * kLn2; }
 };
@@ -233,6 +358,13 @@ struct F32Pack {
   __device__ __forceinline__ static void cols(const T* tile, const float (&p)[16], f32x16 (&acc)[NA]) {
     product_cols<D>(tile, p, acc);
   }
+  __device__ __forceinline__ static void cols_kept(const T* tile, const float (&p)[16], const uint32_t (&w)[8],
+                                                   uint32_t, int thr, f32x16 (&acc)[NA]) {
+    float z[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) z[r] = kept(w, r, thr) ? p[r] : 0.0f;
+    cols(tile, z, acc);
+  }
   template <typename F>
   __device__ __forceinline__ static void features(const f32x16 (&acc)[NA], F put) { for_features<D>(acc, put); }
   __device__ __forceinline__ static void store4(T* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
@@ -241,25 +373,38 @@ struct F32Pack {
   __device__ __forceinline__ static float operand_mul(const PackArgs& a, bool cap) {
     return cap ? a.scale / a.cap : a.scale;
   }
-  __device__ __forceinline__ static ScoreConst consts(const PackArgs& a, bool) { return {1.0f, 0.0f, a.cap}; }
+  __device__ __forceinline__ static ScoreConst consts(const PackArgs& a, bool) {
+    ScoreConst c{};
+    c.cap = a.cap;
+    return c;
+  }
   __device__ __forceinline__ static float entry(float bias, const PackArgs&, bool) {
     return bias <= kNoScore ? -INFINITY : bias;
   }
-  static constexpr float kSlope = 1.0f;
-  // tanh by its series up to 0.3 (next term 5e-8 of it), else 1 - 2 / (e^(2 y) + 1),
-  // off by about 2^-23 against a value of at least 0.29.
-  template <bool CAP>
-  __device__ __forceinline__ static float score(float y, float bias, const ScoreConst& c, float& slope) {
-    if constexpr (!CAP) return y + bias;
-    const float y2 = y * y;
-    const float small = y * fmaf(y2, fmaf(y2, fmaf(y2, fmaf(y2, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f),
-                                          -1.0f / 3.0f), 1.0f);
-    const float big = fmaf(-2.0f, 1.0f / (exp2_fast(fabsf(y) * (2.0f * kLog2e)) + 1.0f), 1.0f);
-    const float t = fabsf(y) < 0.3f ? small : copysignf(big, y);
-    slope = fmaf(-t, t, 1.0f);
-    return fmaf(c.cap, t, bias);
+  // x = S. (The entries are added after the product: as the accumulator's
+  // start they would raise the rounding of every step.) tanh by its series up to
+  // 0.3 (next term 5e-8 of it), else 1 - 2 / (e^(2 y) + 1), off by about 2^-23 against a
+  // value of at least 0.29.
+  template <bool CAP, bool SLOPE>
+  __device__ __forceinline__ static void scores(const f32x16& s, float (&x)[16], float (&slope)[16],
+                                                const ScoreConst& c) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      if constexpr (!CAP) {
+        x[r] += s[r];
+      } else {
+        const float y = s[r], y2 = y * y;
+        const float small = y * fmaf(y2, fmaf(y2, fmaf(y2, fmaf(y2, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f),
+                                              -1.0f / 3.0f), 1.0f);
+        const float big = fmaf(-2.0f, 1.0f / (exp2_fast(fabsf(y) * (2.0f * kLog2e)) + 1.0f), 1.0f);
+        const float t = fabsf(y) < 0.3f ? small : copysignf(big, y);
+        if constexpr (SLOPE) slope[r] = fmaf(-t, t, 1.0f);
+        x[r] = fmaf(c.cap, t, x[r]);
+      }
+    }
   }
-  __device__ __forceinline__ static float expo(float x, float mneg) { return exp2_fast((x + mneg) * kLog2e); }
+  static constexpr float kSlope = 1.0f;
+  __device__ __forceinline__ static float expo(float x) { return exp2_fast(x * kLog2e); }
   __device__ __forceinline__ static float to_unit(float lse) { return lse; }
   __device__ __forceinline__ static float log_sum(float m, float l) { return m + logf(l); }
 };
@@ -295,6 +440,40 @@ struct PackStage {
   }
 };
 
+// bf16: straight to LDS (buffer_load_dwordx4 ... lds), 1 KiB per instruction; the
+// lane that fills chunk c of a row reads the chunk that the swizzle keeps there.
+template <class M>
+struct PackDma {
+  static constexpr int ROWB = M::D * 2;
+  static constexpr int N = 32 * ROWB / 1024;         // instructions per tile
+  uint32_t voff[N];
+  __device__ __forceinline__ explicit PackDma(int64_t rs) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int u = i * 64 + lane, row = u / M::CPR;
+      const int ch = swz_tile<M::D>(row, u % M::CPR);
+      voff[i] = ch < M::DCH ? (uint32_t)row * ((uint32_t)rs * 2u) + (uint32_t)ch * 16u : kZeroChunk;
+    }
+  }
+  // Rows [r0, r0 + 32) of a graph's `rows` rows from p on (rows past them zero).
+  __device__ __forceinline__ void load(const uint16_t* p, int64_t rs, int64_t r0, int64_t rows, uint16_t* tile) const {
+    const int64_t n = rows - r0 < 32 ? rows - r0 : 32;
+    const __amdgpu_buffer_rsrc_t rc = make_rsrc_n(p + r0 * rs, n > 0 ? (n - 1) * rs * 2 + M::DS * 2 : 0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      // (device pass only: see TileDma)
+#if __HIP_DEVICE_COMPILE__
+      typedef __attribute__((address_space(3))) void* lds_void;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rc, (lds_void)(void*)(tile + i * 512), 16, voff[i], 0, 0, 0);
+#else
+      (void)rc;
+      (void)tile;
+#endif
+    }
+  }
+};
+
 // The workgroup's job and head, the wave's group. Workgroups go to the 8 XCDs
 // round robin: with many jobs, a job's heads, which share its distances, stay on
 // one XCD, and the jobs, longest first, are dealt over the XCDs in turn.
@@ -317,9 +496,27 @@ struct PackPlace {
   }
 };
 
+// A record of the plan in scalar registers.
+template <typename T>
+__device__ __forceinline__ T scalar_record(const T* p) {
+  T r = *p;
+  int w[sizeof(T) / 4];
+  __builtin_memcpy(w, &r, sizeof(T));
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(T) / 4); ++i) w[i] = uniform(w[i]);
+  __builtin_memcpy(&r, w, sizeof(T));
+  return r;
+}
+
 template <typename T>
 __device__ __forceinline__ T* rows_at(const PackTensor& t, int h, int64_t row) {
   return reinterpret_cast<T*>(t.p) + h * t.hs + row * t.rs;
+}
+
+// x[r] where r < rem, else fill.
+__device__ __forceinline__ void keep_below(float (&x)[16], int rem, float fill) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) x[r] = r < rem ? x[r] : fill;
 }
 
 // The distances of a query-stationary wave: the lane's row, groups of 16 keys
@@ -334,8 +531,8 @@ struct PackSpdRow {
     const int64_t n = rows < 32 ? rows : 32;
     const uint32_t rem = (uint32_t)(reinterpret_cast<uintptr_t>(first) & 15u);
     const int64_t i = (lane & 31) < n ? (lane & 31) : n - 1;
-    base = first - rem;
-    range = rsrc_range(((n - 1) * ld + nk + rem + 3) & ~(int64_t)3);
+    base = uniform(first - rem);
+    range = uniform(rsrc_range(((n - 1) * ld + nk + rem + 3) & ~(int64_t)3));
     voff = (uint32_t)(i * ld) + 16u * (uint32_t)(lane >> 5) + rem;
     sh = voff & 3u;
     voff -= sh;

@@ -7,17 +7,18 @@
 // with P and dU taken from registers (1 / (1 - p) and scale at the end).
 //
 // Dropout: a lane draws for one query and 16 keys, as the query-stationary kernels
-// do (a draw serves 8 keys of one row). The comparison of key e gives a ballot
-// whose halves are the kept queries of keys e and 16 + e; written to those lanes
-// and exchanged between the halves, each lane has its key's 32 queries as bits.
+// do (a draw serves 8 keys of one row); the kept pairs, a byte each, are transposed
+// through LDS with the 8-bit transposing reads, as the distances are. In dS the
+// 1 / (1 - p) of dP is left out: dS (1 - p) = P (z dP - D (1 - p)).
 //
 // Table gradient: dS is added into an LDS histogram in fixed point, 64-bit sums of
 // round(dS 2^F) (float adds to LDS are some twenty times slower), in 32 copies
 // (lane & 31) of up to 128 buckets or 16 of 256. F comes from the largest
 // |dS| that the dQ kernel met in this head, so that every term stays below 2^31
-// and the rounding of 2^-31 of it is far below the sums in fp32. Each workgroup
-// writes its sums; a last kernel adds them in a fixed order. Everything is
-// bitwise reproducible.
+// and the rounding of 2^-31 of it is far below the sums in fp32; V's operand and
+// the staged D carry it, so that dS arrives scaled. Each workgroup writes its
+// sums; a last kernel adds them in a fixed order. Everything is bitwise
+// reproducible.
 #pragma once
 #include "pack.hpp"
 
@@ -27,52 +28,61 @@ namespace {
 
 constexpr int kPackHist = 4096;
 
-// v_writelane_b32 (this compiler has the intrinsic, but no builtin for it): old
-// with `lane` set to the wave-uniform val.
-__device__ uint32_t write_lane(uint32_t val, uint32_t lane, uint32_t old) __asm("llvm.amdgcn.writelane.i32");
-
-// Bits of the queries that keep the lane's key, from the draws of the lane's
-// query (lane & 31) for keys 16 g .. + 15: bit r is query 16 g + r.
-__device__ __forceinline__ uint32_t kept_queries(const uint32_t (&rw)[8], int thr) {
-  const int lane = threadIdx.x & 63;
-  uint32_t bits = 0;
-#pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const uint64_t b = __builtin_amdgcn_ballot_w64(kept(rw, e, thr));
-    bits = write_lane((uint32_t)b, e, bits);
-    bits = write_lane((uint32_t)(b >> 32), 16 + e, bits);
-  }
-  bits = __shfl(bits, lane & 31);
-  return bits >> (16 * (lane >> 5));
+__device__ __forceinline__ int pack_round(float x) {
+  int r;
+  asm("v_cvt_rpi_i32_f32 %0, %1" : "=v"(r) : "v"(x));   // floor(x + 0.5)
+  return r;
 }
 
-template <class M, bool CAP, bool DROP>
+// 32 x 32 bytes of a wave, 16 per lane row by row (lane l: row l / 2, from column
+// 16 (l & 1) on, or row l & 31, from column 16 (l >> 5) on), to the lane's column
+// (lane & 31), rows 16 g + 0 .. 15.
+__device__ __forceinline__ void transpose_bytes(uint8_t* st, int at, uint4 v, const int (&off_tr8)[2], uint32_t (&b)[4]) {
+  typedef int i32x2 __attribute__((ext_vector_type(2)));
+  typedef __attribute__((address_space(3))) i32x2* lds_i32x2;
+  *reinterpret_cast<uint4*>(st + at) = v;
+#pragma unroll
+  for (int hh = 0; hh < 2; ++hh) {
+    const i32x2 x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2)(void*)(st + off_tr8[hh]));
+    b[2 * hh] = (uint32_t)x.x;
+    b[2 * hh + 1] = (uint32_t)x.y;
+  }
+}
+
+// WIDE: more than 127 buckets (the narrow layout keeps bucket 127 for the bytes
+// past it).
+template <class M, bool CAP, bool DROP, bool WIDE>
 __global__ __launch_bounds__(kPackThreads, 2) void pack_dkdv_kernel(PackArgs a) {
   using T = typename M::T;
   constexpr int NA = M::NA;
+  // staged tiles: two where both fit beside the histogram twice per compute unit
+  constexpr int NB = M::BF16 && M::D == 32 ? 2 : 1;
   constexpr int XCH = NA * 16 * 64 * 4 * 2;
   constexpr int STG = 2 * kPackWaves * M::TILE * (int)sizeof(T);
-  __shared__ alignas(128) uint8_t sBuf[STG > XCH ? STG : XCH];
-  __shared__ alignas(16) unsigned long long hist[kPackHist];
-  __shared__ float sTab[256];
-  __shared__ alignas(16) float sStat[kPackWaves][64];     // per staged row: -LSE; D
-  __shared__ alignas(16) uint8_t sSpd[kPackWaves][1024];
+  constexpr int CPY = WIDE ? 16 : 32;
+  // (LDS objects are placed by decreasing alignment: the table and the histogram
+  // first, where a DS immediate of 16 bits reaches them)
+  __shared__ alignas(4096) float sTab[256];
+  __shared__ alignas(2048) unsigned long long hist[kPackHist];
+  __shared__ alignas(1024) uint8_t sByte[kPackWaves][1024];
+  __shared__ alignas(512) float sStat[NB][kPackWaves][64]; // per staged row: -LSE; D (1 - p) 2^F, negative without dropout
+  __shared__ alignas(128) uint8_t sBuf0[STG > XCH ? STG : XCH];
+  __shared__ alignas(128) uint8_t sBuf1[NB == 2 ? STG : 16];
   __shared__ float red[2][kPackWaves];
   __shared__ int bad[kPackWaves];
-  T* sQ = reinterpret_cast<T*>(sBuf);
-  T* sO = sQ + kPackWaves * M::TILE;
 
   const PackPlace pl(a);
   if (pl.job >= a.njobs) return;
   const int h = pl.h;
-  const PackJob jb = a.jobs[pl.job];
+  const PackJob jb = scalar_record(a.jobs + pl.job);
   const int tid = threadIdx.x, wave = wave_id(), lane = tid & 63, col = lane & 31, g = lane >> 5;
   const int lw = jb.log2w, W = 1 << lw;
   const int grp = wave >> lw, gw = wave & (W - 1);
-  const PackGroup gr = a.groups[jb.group + grp];
-  const bool wide = a.n_buckets > 127;
-  sTab[tid] = M::entry(tid < a.n_buckets ? a.table[(int64_t)h * a.n_buckets + tid] : 0.0f, a, CAP);
-  for (int t = tid; t < kPackHist / 2; t += kPackThreads) reinterpret_cast<uint4*>(hist)[t] = make_uint4(0u, 0u, 0u, 0u);
+  const PackGroup gr = scalar_record(a.groups + jb.group + grp);
+  sTab[tid] = M::entry(tid < a.n_buckets ? a.table[(int64_t)h * a.n_buckets + tid] : 0.0f, a, false)
+              + (M::BF16 && CAP ? a.cap * kLog2e : 0.0f);
+  for (int t = tid; t < kPackHist / 2; t += kPackThreads)
+    if (t < a.n_buckets * CPY / 2) reinterpret_cast<uint4*>(hist)[t] = make_uint4(0u, 0u, 0u, 0u);
   {
     const float2* dm = a.dmax + (int64_t)h * a.njobs_dq * kPackWaves;
     float x = 0.0f, y = 0.0f;
@@ -105,7 +115,7 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_dkdv_kernel(PackArgs a) 
     int e;
     frexpf(bound, &e);                                    // bound < 2^e
     fexp = 30 - e;
-    fexp = fexp > 100 ? 100 : (fexp < -90 ? -90 : fexp);
+    fexp = fexp > 60 ? 60 : (fexp < -60 ? -60 : fexp);
   }
   const float sF = ldexpf(1.0f, fexp);
 
@@ -125,9 +135,19 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_dkdv_kernel(PackArgs a) 
   const float* dlth = a.dlt + h * a.ld_dlt + gr.q0;
   typename M::Operand k, v;
   M::load_operand(rows_at<const T>(a.k, h, gr.k0 + jc), active, M::operand_mul(a, CAP), k);
-  M::load_operand(rows_at<const T>(a.v, h, gr.k0 + jc), active, 1.0f, v);
+  M::load_operand(rows_at<const T>(a.v, h, gr.k0 + jc), active, sF, v);
   const ScoreConst sc = M::consts(a, CAP);
-  const uint32_t roff = DROP ? a.offset + (a.offset_dev ? *a.offset_dev : 0u) : 0u;
+  // uncapped bf16: the score accumulator starts from -LSE log2 e / mul
+  constexpr bool START = M::BF16 && !CAP;
+  const float ml_mul = START ? 1.0f / sc.mul : 1.0f;
+  const float d_mul = DROP ? sF : -sF;
+  const Philox rng(a, h);
+  uint4 rk0{}, rk1{};
+  if constexpr (DROP) {
+    rk0 = rng.keys((uint32_t)(jw + 16 * g) / 8u);
+    rk1 = rng.keys((uint32_t)(jw + 16 * g) / 8u + 1u);
+  }
+  const uint32_t below = (uint32_t)((a.thr - 1) & 0xffff) * 0x10001u;
 
   f32x16 dk[NA], dv[NA];
 #pragma unroll
@@ -154,111 +174,175 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_dkdv_kernel(PackArgs a) 
   for (int hh = 0; hh < 2; ++hh)
     off_tr8[hh] = (16 * g + 8 * hh + ((lane & 15) >> 1)) * 32 + 16 * ((lane >> 4) & 1) + 8 * (lane & 1);
 
-  PackStage<M> tq, to;
-  float stat = 0.0f;
   uint32_t w[5];
   const int step = 32 << lw;
-  int t0 = gr.c0;
-  auto load = [&](int i0) {
-    tq.load(qh, a.q.rs, i0, gr.nq);
-    to.load(oh, a.d_o.rs, i0, gr.nq);
+  float stat = 0.0f;
+  auto load_stat = [&](int i0) {
     const int r = i0 + col < gr.nq ? i0 + col : gr.nq - 1;
     if (gr.nq > 0) stat = (g == 0 ? lseh : dlth)[r];
   };
-  auto store = [&](int i0) {
-    tq.store(sQ + wave * M::TILE);
-    to.store(sO + wave * M::TILE);
+  auto store_stat = [&](int i0, int buf) {
     float x = stat;
     opaque_f(x);
     const bool in = i0 + col < gr.nq;
     if (g == 0)
-      x = in && x != -INFINITY ? -M::to_unit(x) : -INFINITY;
+      x = in && x != -INFINITY ? -M::to_unit(x) * ml_mul : -INFINITY;
     else
-      x = in ? x : 0.0f;
-    sStat[wave][lane] = x;
+      x = in ? x * d_mul : 0.0f;
+    sStat[buf][wave][lane] = x;
   };
-  if (jb.steps > 0) {
-    load(t0 + gw * 32);
-    fetch(t0, w);
-  }
-  for (int t = 0; t < jb.steps; ++t, t0 += step) {
-    lds_barrier();
-    store(t0 + gw * 32);
-    lds_barrier();
-    if (t + 1 < jb.steps) load(t0 + step + gw * 32);
-    if (!active) continue;
-    for (int ib = 0; ib < W; ++ib) {
-      const int i0 = t0 + ib * 32;
-      if (i0 >= gr.c1) break;
-      const int slot = (grp << lw) + ib;
-      align_spd5(w, ssh);
-      uint4 w4 = make_uint4(w[0], w[1], w[2], w[3]);
-      fetch(i0 + 32, w);
-      if (i0 + 31 < lo0) continue;                        // no query of the block sees a key (wave-uniform)
-      *reinterpret_cast<uint4*>(&sSpd[wave][16 * lane]) = w4;
-      uint32_t b[4];
+
+  // One block of 32 queries from i0 on, staged in qt and ot.
+  auto block = [&](const T* qt, const T* ot, const float* st, int i0) {
+    align_spd5(w, ssh);
+    const uint4 w4 = make_uint4(w[0], w[1], w[2], w[3]);
+    fetch(i0 + 32, w);
+    if (i0 + 31 < lo0) return;                            // no query of the block sees a key (wave-uniform)
+    uint32_t b[4];
+    transpose_bytes(sByte[wave], 16 * lane, w4, off_tr8, b);
+    f32x16 s, dp;
+    float x[16], slope[16], ml[16], dl[16];
 #pragma unroll
-      for (int hh = 0; hh < 2; ++hh) {
-        typedef int i32x2 __attribute__((ext_vector_type(2)));
-        typedef __attribute__((address_space(3))) i32x2* lds_i32x2;
-        const i32x2 x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2)(void*)&sSpd[wave][off_tr8[hh]]);
-        b[2 * hh] = (uint32_t)x.x;
-        b[2 * hh + 1] = (uint32_t)x.y;
-      }
-      f32x16 s = zero_f32x16(), dp = zero_f32x16();
-      M::rows(sQ + slot * M::TILE, k, s);
-      M::rows(sO + slot * M::TILE, v, dp);
-      float x[16], slope[16], p[16], ml[16], dl[16];
-      bias16(sTab, b, x);
+    for (int u = 0; u < 4; ++u) {
+      const float4 y = *reinterpret_cast<const float4*>(st + 16 * g + 4 * u);
+      const float4 z = *reinterpret_cast<const float4*>(st + 32 + 16 * g + 4 * u);
+      ml[4 * u] = y.x; ml[4 * u + 1] = y.y; ml[4 * u + 2] = y.z; ml[4 * u + 3] = y.w;
+      dl[4 * u] = z.x; dl[4 * u + 1] = z.y; dl[4 * u + 2] = z.z; dl[4 * u + 3] = z.w;
+    }
+    bias16(sTab, b, x);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const float4 y = *reinterpret_cast<const float4*>(&sStat[slot][16 * g + 4 * u]);
-        const float4 z = *reinterpret_cast<const float4*>(&sStat[slot][32 + 16 * g + 4 * u]);
-        ml[4 * u] = y.x; ml[4 * u + 1] = y.y; ml[4 * u + 2] = y.z; ml[4 * u + 3] = y.w;
-        dl[4 * u] = z.x; dl[4 * u + 1] = z.y; dl[4 * u + 2] = z.z; dl[4 * u + 3] = z.w;
-      }
+    for (int r = 0; r < 16; ++r) {
+      s[r] = START ? ml[r] : 0.0f;
+      dp[r] = DROP ? 0.0f : dl[r];
+    }
+    M::rows(qt, k, s);
+    M::rows(ot, v, dp);
+    if constexpr (START) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        x[r] = M::template score<CAP>(s[r], x[r], sc, slope[r]);
-        p[r] = M::expo(x[r], ml[r]);
-      }
-      if (i0 < lo1 || jw + 32 > gr.nk) {
-        const int r0 = lo - i0 - 16 * g;
+      for (int r = 0; r < 16; ++r) x[r] = fmaf(s[r], sc.mul, x[r]);
+    } else {
+      M::template scores<CAP, true>(s, x, slope, sc);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) p[r] = jok && r >= r0 ? p[r] : 0.0f;
-      }
-      uint32_t keep = 0;
-      if constexpr (DROP) {
-        uint32_t rw[8];
-        draw16(a, roff, h, (uint32_t)(gr.q0 + i0 + col), jw + 16 * g, rw);
-        keep = kept_queries(rw, a.thr);
-      }
+      for (int r = 0; r < 16; ++r) x[r] += ml[r];
+    }
+    float p[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) p[r] = M::expo(x[r]);
+    if (i0 < lo1 || jw + 32 > gr.nk) {
+      const int r0 = jok ? lo - i0 - 16 * g : 16;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) p[r] = r >= r0 ? p[r] : 0.0f;
+    }
+    if constexpr (DROP) {
+      uint32_t rw[8], z[4];
+      const RowDraw rr = rng.row((uint32_t)(gr.q0 + i0 + col));
+      rng.draw(rr, rk0, rw);
+      rng.draw(rr, rk1, rw + 4);
+      uint4 kb;
+      kb.x = __builtin_amdgcn_perm(kept2(rw[1], below), kept2(rw[0], below), 0x06040200u) & 0x01010101u;
+      kb.y = __builtin_amdgcn_perm(kept2(rw[3], below), kept2(rw[2], below), 0x06040200u) & 0x01010101u;
+      kb.z = __builtin_amdgcn_perm(kept2(rw[5], below), kept2(rw[4], below), 0x06040200u) & 0x01010101u;
+      kb.w = __builtin_amdgcn_perm(kept2(rw[7], below), kept2(rw[6], below), 0x06040200u) & 0x01010101u;
+      transpose_bytes(sByte[wave], 32 * col + 16 * g, kb, off_tr8, z);
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        float d = dp[r];
-        if constexpr (DROP) d = (keep >> r) & 1u ? d * a.rp : 0.0f;
-        x[r] = p[r] * (d - dl[r]);
-        if constexpr (DROP) p[r] = (keep >> r) & 1u ? p[r] : 0.0f;
+        const float pz = p[r] * (float)((z[r >> 2] >> (8 * (r & 3))) & 0xffu);
+        x[r] = fmaf(pz, dp[r], -p[r] * dl[r]);
+        p[r] = pz;
       }
-      if (!wide && __any(((b[0] | b[1] | b[2] | b[3]) & 0x80808080u) != 0)) {
-        // the narrow layout ends at 127, which is past its buckets
+    } else {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] = p[r] * dp[r];
+    }
+    if constexpr (!WIDE) {
+      if (__any(((b[0] | b[1] | b[2] | b[3]) & 0x80808080u) != 0)) {     // past the narrow layout: to 127
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           const uint32_t hi = (b[u] >> 7) & 0x01010101u;
           b[u] = (b[u] | hi * 0x7fu) & 0x7f7f7f7fu;
         }
       }
-      const int sh = wide ? 7 : 8;
-      const uint32_t copy = (uint32_t)(lane & (wide ? 15 : 31)) * 8u;
+    }
+    const uint32_t copy = (uint32_t)(lane & (CPY - 1)) * 8u;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const uint32_t at = (((b[r >> 2] >> (8 * (r & 3))) & 0xffu) << sh) | copy;
-        atomicAdd(reinterpret_cast<unsigned long long*>(reinterpret_cast<uint8_t*>(hist) + at),
-                  (unsigned long long)(long long)__float2int_rn(x[r] * sF));
-        if constexpr (CAP) x[r] *= slope[r];
+    for (int r = 0; r < 16; ++r) {
+      const uint32_t at = WIDE ? ((((b[r >> 2] >> (8 * (r & 3))) & 0xffu) << 7) | copy)
+                               : __builtin_amdgcn_perm(b[r >> 2], copy, 0x0c0c0000u | ((4u + (r & 3)) << 8));
+      atomicAdd(reinterpret_cast<unsigned long long*>(reinterpret_cast<uint8_t*>(hist) + at),
+                (unsigned long long)(long long)pack_round(x[r]));
+      if constexpr (CAP) x[r] *= slope[r];
+    }
+    M::cols(ot, p, dv);
+    M::cols(qt, x, dk);
+  };
+  auto blocks = [&](const T* sQ, const T* sO, int buf, int t0) {
+    if (!active) return;
+    for (int ib = 0; ib < W; ++ib) {
+      const int i0 = t0 + ib * 32, slot = (grp << lw) + ib;
+      if (i0 >= gr.c1) break;
+      block(sQ + slot * M::TILE, sO + slot * M::TILE, sStat[buf][slot], i0);
+    }
+  };
+
+  int t0 = gr.c0;
+  T* const sQ0 = reinterpret_cast<T*>(sBuf0);
+  T* const sO0 = sQ0 + kPackWaves * M::TILE;
+  if (jb.steps > 0) {
+    load_stat(t0 + gw * 32);
+    fetch(t0, w);
+  }
+  if constexpr (M::BF16) {
+    const PackDma<M> cq(a.q.rs), co(a.d_o.rs);
+    auto stage = [&](T* q, T* o, int buf, int t) {
+      cq.load(qh, a.q.rs, t + gw * 32, gr.nq, q + wave * M::TILE);
+      co.load(oh, a.d_o.rs, t + gw * 32, gr.nq, o + wave * M::TILE);
+      store_stat(t + gw * 32, buf);
+      load_stat(t + step + gw * 32);
+    };
+    if constexpr (NB == 2) {
+      T* const sQ1 = reinterpret_cast<T*>(sBuf1);
+      T* const sO1 = sQ1 + kPackWaves * M::TILE;
+      if (jb.steps > 0) stage(sQ0, sO0, 0, t0);
+      for (int t = 0; t < jb.steps; t += 2) {
+        wait_vmcnt<0>();
+        lds_barrier();
+        if (t + 1 < jb.steps) stage(sQ1, sO1, 1, t0 + step);
+        blocks(sQ0, sO0, 0, t0);
+        t0 += step;
+        if (t + 1 >= jb.steps) break;
+        wait_vmcnt<0>();
+        lds_barrier();
+        if (t + 2 < jb.steps) stage(sQ0, sO0, 0, t0 + step);
+        blocks(sQ1, sO1, 1, t0);
+        t0 += step;
       }
-      M::cols(sO + slot * M::TILE, p, dv);
-      M::cols(sQ + slot * M::TILE, x, dk);
+    } else {
+      for (int t = 0; t < jb.steps; ++t, t0 += step) {
+        lds_barrier();
+        stage(sQ0, sO0, 0, t0);
+        wait_vmcnt<0>();
+        lds_barrier();
+        blocks(sQ0, sO0, 0, t0);
+      }
+    }
+  } else {
+    PackStage<M> tq, to;
+    auto load = [&](int t) {
+      tq.load(qh, a.q.rs, t + gw * 32, gr.nq);
+      to.load(oh, a.d_o.rs, t + gw * 32, gr.nq);
+    };
+    if (jb.steps > 0) load(t0);
+    for (int t = 0; t < jb.steps; ++t, t0 += step) {
+      lds_barrier();
+      tq.store(sQ0 + wave * M::TILE);
+      to.store(sO0 + wave * M::TILE);
+      store_stat(t0 + gw * 32, 0);
+      lds_barrier();
+      if (t + 1 < jb.steps) {
+        load(t0 + step);
+        load_stat(t0 + step + gw * 32);
+      }
+      blocks(sQ0, sO0, 0, t0);
     }
   }
   {
@@ -271,41 +355,50 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_dkdv_kernel(PackArgs a) 
     if (lane == 0) bad[wave] = any_bad;
   }
   if (jb.combine) {
-    float* buf = reinterpret_cast<float*>(sBuf);
+    float* buf = reinterpret_cast<float*>(sBuf0);
     auto none = [](int) {};
     auto add = [](int, float& wa, float& wo) { wa = wo = 1.0f; };
     pack_combine(buf, lw, grp, gw, dk, none, add);
     pack_combine(buf, lw, grp, gw, dv, none, add);
   }
+  const float rp = DROP ? a.rp : 1.0f;
   if (jok && (!jb.combine || grp == 0)) {
-    const float mk = a.scale * (CAP ? M::kSlope : 1.0f), mv = DROP ? a.rp : 1.0f;
+    const float mk = a.scale * rp * ldexpf(1.0f, -fexp) * (CAP ? M::kSlope : 1.0f);
     T* dkp = rows_at<T>(a.dk, h, gr.k0 + j);
     T* dvp = rows_at<T>(a.dv, h, gr.k0 + j);
     M::features(dk, [&](int f, float4 x) { M::store4(dkp + f, make_float4(x.x * mk, x.y * mk, x.z * mk, x.w * mk)); });
-    M::features(dv, [&](int f, float4 x) { M::store4(dvp + f, make_float4(x.x * mv, x.y * mv, x.z * mv, x.w * mv)); });
+    M::features(dv, [&](int f, float4 x) { M::store4(dvp + f, make_float4(x.x * rp, x.y * rp, x.z * rp, x.w * rp)); });
   }
   __syncthreads();
-  const int cpy = wide ? 16 : 32;
-  const double unscale = ldexp(1.0, -fexp);
+  const double unscale = ldexp((double)rp, -fexp);
   const bool nan = bad[0] | bad[1] | bad[2] | bad[3];
   for (int b = tid; b < a.n_buckets; b += kPackThreads) {
     long long t = 0;
-    for (int c = 0; c < cpy; ++c) t += (long long)hist[b * cpy + ((c + b) & (cpy - 1))];
+#pragma unroll
+    for (int c = 0; c < CPY; ++c) t += (long long)hist[b * CPY + ((c + b) & (CPY - 1))];
     a.dtab_part[((int64_t)h * a.njobs + pl.job) * a.n_buckets + b] = nan ? (double)NAN : (double)t * unscale;
   }
 }
 
+template <class M, bool CAP, bool DROP>
+void launch_pack_dkdv_nb(const PackArgs& a, hipStream_t s) {
+  const dim3 grid(pack_grid(a.njobs, a.H)), block(kPackThreads);
+  if (a.n_buckets > 127)
+    hipLaunchKernelGGL((pack_dkdv_kernel<M, CAP, DROP, true>), grid, block, 0, s, a);
+  else
+    hipLaunchKernelGGL((pack_dkdv_kernel<M, CAP, DROP, false>), grid, block, 0, s, a);
+}
+
 template <class M>
 hipError_t launch_pack_dkdv(const PackArgs& a, bool cap, bool drop, hipStream_t s) {
-  const dim3 grid(pack_grid(a.njobs, a.H)), block(kPackThreads);
   if (cap && drop)
-    hipLaunchKernelGGL((pack_dkdv_kernel<M, true, true>), grid, block, 0, s, a);
+    launch_pack_dkdv_nb<M, true, true>(a, s);
   else if (cap)
-    hipLaunchKernelGGL((pack_dkdv_kernel<M, true, false>), grid, block, 0, s, a);
+    launch_pack_dkdv_nb<M, true, false>(a, s);
   else if (drop)
-    hipLaunchKernelGGL((pack_dkdv_kernel<M, false, true>), grid, block, 0, s, a);
+    launch_pack_dkdv_nb<M, false, true>(a, s);
   else
-    hipLaunchKernelGGL((pack_dkdv_kernel<M, false, false>), grid, block, 0, s, a);
+    launch_pack_dkdv_nb<M, false, false>(a, s);
   return hipGetLastError();
 }
 

@@ -4,10 +4,13 @@
 // Query-stationary as the forward: S^T = K Q^T, dP^T = V dO^T, P = exp(S - LSE),
 //   dS = P (z dP / (1 - p) - D),   D_i = dO_i . O_i,
 //   dU = dS (1 - tanh^2),   dQ^T += K^T dU^T, times scale at the end.
-// D from the rounded O is off by O's rounding, which the table gradient, a sum in
-// fp32, would show. The sum of a row's dS is zero with the exact D, so with
-// D0 = dO . O the kernel's own sum of dS is D - D0: the row sum written for the
-// dK / dV kernel is D0 plus it. (dQ itself is rounded as O is, and takes D0.)
+// D from a bf16 O is off by O's rounding: the table gradient, a sum in fp32, would
+// show it, and dQ too where the softmax is peaked, since a row's error is the same
+// for all of its keys (2.6 times the rounding of dQ itself for graphs of some
+// thirty nodes, d = 8). The sum of a row's dS is zero with the exact D, so with
+// D0 = dO . O the kernel's own sum of dS is D - D0. The row sum written for the
+// dK / dV kernel is D0 plus it, and dQ is corrected by it times the sum of
+// P (1 - tanh^2) K, which takes a second product per key tile.
 //
 // It also gives the largest |dS| of each wave and the largest correction of D,
 // from which the dK / dV kernel takes the scale of its fixed-point table gradient.
@@ -22,24 +25,35 @@ template <class M, bool CAP, bool DROP>
 __global__ __launch_bounds__(kPackThreads, 2) void pack_dq_kernel(PackArgs a) {
   using T = typename M::T;
   constexpr int NA = M::NA;
+  constexpr int NB = M::BF16 ? 2 : 1;                            // staged tiles
+  constexpr bool FIX = M::BF16;                                  // dQ is corrected for O's rounding
   constexpr int XCH = NA * 16 * 64 * 4 * 2 + 2 * 64 * 8;
   constexpr int STG = 2 * kPackWaves * M::TILE * (int)sizeof(T);
-  __shared__ alignas(128) uint8_t sBuf[STG > XCH ? STG : XCH];
+  __shared__ alignas(128) uint8_t sBuf0[STG > XCH ? STG : XCH];
+  __shared__ alignas(128) uint8_t sBuf1[NB == 2 ? STG : 16];
   __shared__ float sTab[256];
-  T* sK = reinterpret_cast<T*>(sBuf);
-  T* sV = sK + kPackWaves * M::TILE;
+  __shared__ uint4 sKeys[DROP ? NB * kPackWaves * 4 : 1];
 
   const PackPlace pl(a);
   if (pl.job >= a.njobs) return;
   const int h = pl.h;
-  const PackJob jb = a.jobs[pl.job];
+  const PackJob jb = scalar_record(a.jobs + pl.job);
   const int wave = wave_id(), lane = threadIdx.x & 63, col = lane & 31, g = lane >> 5;
   const int lw = jb.log2w, W = 1 << lw;
   const int grp = wave >> lw, gw = wave & (W - 1);
-  const PackGroup gr = a.groups[jb.group + grp];
+  const PackGroup gr = scalar_record(a.groups + jb.group + grp);
+  constexpr bool START = M::BF16 && !CAP;
+  ScoreRef ref{false, 0.0f};
   {
     const int b = threadIdx.x;
-    sTab[b] = M::entry(b < a.n_buckets ? a.table[(int64_t)h * a.n_buckets + b] : 0.0f, a, CAP);
+    float e = M::entry(b < a.n_buckets ? a.table[(int64_t)h * a.n_buckets + b] : 0.0f, a, START);
+    if constexpr (M::BF16 && CAP) {
+      const float cap2 = a.cap * kLog2e;
+      ref = score_ref(e, cap2, reinterpret_cast<float*>(sBuf0));
+      e += cap2 - ref.ref;
+      __syncthreads();
+    }
+    sTab[b] = e;
   }
 
   const int off = gr.nk - gr.nq;
@@ -59,107 +73,192 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_dq_kernel(PackArgs a) {
   typename M::Operand q, d_o;
   M::load_operand(rows_at<const T>(a.q, h, gr.q0 + ic), active, M::operand_mul(a, CAP), q);
   M::load_operand(rows_at<const T>(a.d_o, h, gr.q0 + ic), active && iok, 1.0f, d_o);
-  float dlt, mlse;                                     // D0 and -LSE (-inf: every P of the row is 0)
+  // D0 and -LSE (-inf: every P of the row is 0). With dropout the 1 / (1 - p) of dP is
+  // left out up to the end: dS (1 - p) = P (z dP - D (1 - p)).
+  const float rp = DROP ? a.rp : 1.0f;
+  float dlt, mlse;
   {
     typename M::Operand o;
     M::load_operand(rows_at<const T>(a.o, h, gr.q0 + ic), active && iok, 1.0f, o);
     dlt = M::dot(o, d_o);
-    dlt += __shfl_xor(dlt, 32);
+    dlt = (dlt + __shfl_xor(dlt, 32)) / rp;
     const float lse = active && iok ? a.lse[h * a.ld_lse + gr.q0 + ic] : -INFINITY;
     mlse = lse == -INFINITY ? -INFINITY : -M::to_unit(lse);
   }
   const ScoreConst sc = M::consts(a, CAP);
-  const uint32_t roff = DROP ? a.offset + (a.offset_dev ? *a.offset_dev : 0u) : 0u;
+  const Philox rng(a, h);
+  RowDraw rrow{};
+  if constexpr (DROP) rrow = rng.row((uint32_t)(gr.q0 + i));
   const PackSpdRow spd(a.spd + gr.spd + (int64_t)(active ? iw : 0) * gr.ld, gr.ld, active ? gr.nq - iw : 1,
                        active ? gr.nk : 0);
-  f32x16 acc[NA];
+  f32x16 acc[NA], fix[NA];
 #pragma unroll
-  for (int c = 0; c < NA; ++c) acc[c] = zero_f32x16();
+  for (int c = 0; c < NA; ++c) {
+    acc[c] = zero_f32x16();
+    fix[c] = zero_f32x16();
+  }
   float dsum = 0.0f, dmax = 0.0f;
-
-  PackStage<M> tk, tv;
   uint32_t w[5];
   const int step = 32 << lw;
-  int t0 = gr.c0;
-  if (jb.steps > 0) {
-    tk.load(kh, a.k.rs, t0 + gw * 32, gr.nk);
-    tv.load(vh, a.v.rs, t0 + gw * 32, gr.nk);
-    spd.fetch(t0, w);
-  }
-  for (int t = 0; t < jb.steps; ++t, t0 += step) {
-    lds_barrier();
-    tk.store(sK + wave * M::TILE);
-    tv.store(sV + wave * M::TILE);
-    lds_barrier();
-    if (t + 1 < jb.steps) {
-      tk.load(kh, a.k.rs, t0 + step + gw * 32, gr.nk);
-      tv.load(vh, a.v.rs, t0 + step + gw * 32, gr.nk);
+
+  auto block = [&](const T* kt, const T* vt, const uint4* keys, int j0) {
+    align_spd5(w, spd.sh);
+    float x[16], slope[16];
+    bias16(sTab, w, x);
+    spd.fetch(j0 + 32, w);
+    f32x16 s = zero_f32x16(), dp;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      if constexpr (START) s[r] = x[r];
+      dp[r] = DROP ? 0.0f : -dlt;
     }
+    M::rows(kt, q, s);
+    M::rows(vt, d_o, dp);
+    if constexpr (START) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] = fmaf(s[r], sc.mul, mlse);
+    } else {
+      M::template scores<CAP, true>(s, x, slope, sc);
+      if (!ref.fixed) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[r] += mlse;
+      }
+    }
+    if (j0 + 32 > lim0) keep_below(x, lim - j0 - 16 * g, -INFINITY);
+    if constexpr (DROP) {
+      uint32_t rw[8];
+      rng.draw(rrow, keys[2 * g], rw);
+      rng.draw(rrow, keys[2 * g + 1], rw + 4);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dp[r] = (kept(rw, r, a.thr) ? dp[r] : 0.0f) - dlt;
+    }
+    float du[16];
+    float bsum = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) {
+#pragma unroll
+      for (int e = r; e < r + 2; ++e) {
+        x[e] = M::expo(x[e]);
+        const float ds = x[e] * dp[e];
+        bsum += ds;
+        if constexpr (CAP) x[e] *= slope[e];
+        du[e] = CAP ? x[e] * dp[e] : ds;
+        s[e] = ds;
+      }
+      dmax = fmaxf(fmaxf(dmax, fabsf(s[r])), fabsf(s[r + 1]));
+    }
+    dsum += bsum;
+    if constexpr (FIX)
+      M::cols2(kt, du, acc, x, fix);
+    else
+      M::cols(kt, du, acc);
+  };
+  auto put_keys = [&](int t0, int buf) {
+    if constexpr (DROP) {
+      const uint4 k = rng.keys((uint32_t)(t0 + gw * 32) / 8u + (uint32_t)(lane & 3));
+      if (lane < 4) sKeys[(buf * kPackWaves + wave) * 4 + lane] = k;
+    }
+  };
+  auto blocks = [&](const T* sK, const T* sV, int buf, int t0) {
     for (int kb = 0; kb < W; ++kb) {
-      const int j0 = t0 + kb * 32;
+      const int j0 = t0 + kb * 32, slot = (grp << lw) + kb;
       if (j0 >= lim1) break;
-      const T* kt = sK + ((grp << lw) + kb) * M::TILE;
-      const T* vt = sV + ((grp << lw) + kb) * M::TILE;
-      align_spd5(w, spd.sh);
-      float x[16], slope[16];
-      bias16(sTab, w, x);
-      spd.fetch(j0 + 32, w);
-      f32x16 s = zero_f32x16(), dp = zero_f32x16();
-      M::rows(kt, q, s);
-      M::rows(vt, d_o, dp);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) x[r] = M::template score<CAP>(s[r], x[r], sc, slope[r]);
-      if (j0 + 32 > lim0) {
-        const int rem = lim - j0 - 16 * g;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) x[r] = r < rem ? x[r] : -INFINITY;
+      block(sK + slot * M::TILE, sV + slot * M::TILE, sKeys + (DROP ? (buf * kPackWaves + slot) * 4 : 0), j0);
+    }
+  };
+
+  int t0 = gr.c0;
+  T* const sK0 = reinterpret_cast<T*>(sBuf0);
+  T* const sV0 = sK0 + kPackWaves * M::TILE;
+  if (jb.steps > 0) spd.fetch(t0, w);
+  if constexpr (M::BF16) {
+    T* const sK1 = reinterpret_cast<T*>(sBuf1);
+    T* const sV1 = sK1 + kPackWaves * M::TILE;
+    const PackDma<M> dk(a.k.rs), dv(a.v.rs);
+    auto copy = [&](T* k, T* v, int t) {
+      dk.load(kh, a.k.rs, t + gw * 32, gr.nk, k + wave * M::TILE);
+      dv.load(vh, a.v.rs, t + gw * 32, gr.nk, v + wave * M::TILE);
+    };
+    if (jb.steps > 0) {
+      copy(sK0, sV0, t0);
+      put_keys(t0, 0);
+    }
+    for (int t = 0; t < jb.steps; t += 2) {
+      wait_vmcnt<0>();
+      lds_barrier();
+      if (t + 1 < jb.steps) {
+        copy(sK1, sV1, t0 + step);
+        put_keys(t0 + step, 1);
       }
-      if constexpr (DROP) {
-        uint32_t rw[8];
-        draw16(a, roff, h, (uint32_t)(gr.q0 + i), j0 + 16 * g, rw);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) dp[r] = kept(rw, r, a.thr) ? dp[r] * a.rp : 0.0f;
+      blocks(sK0, sV0, 0, t0);
+      t0 += step;
+      if (t + 1 >= jb.steps) break;
+      wait_vmcnt<0>();
+      lds_barrier();
+      if (t + 2 < jb.steps) {
+        copy(sK0, sV0, t0 + step);
+        put_keys(t0 + step, 0);
       }
-      float bsum = 0.0f;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        x[r] = M::expo(x[r], mlse) * (dp[r] - dlt);
-        bsum += x[r];
-        dmax = fmaxf(dmax, fabsf(x[r]));
-        if constexpr (CAP) x[r] *= slope[r];
-      }
-      dsum += bsum;
-      M::cols(kt, x, acc);
+      blocks(sK1, sV1, 1, t0);
+      t0 += step;
+    }
+  } else {
+    PackStage<M> tk, tv;
+    auto load = [&](int t) {
+      tk.load(kh, a.k.rs, t + gw * 32, gr.nk);
+      tv.load(vh, a.v.rs, t + gw * 32, gr.nk);
+    };
+    if (jb.steps > 0) load(t0);
+    for (int t = 0; t < jb.steps; ++t, t0 += step) {
+      lds_barrier();
+      tk.store(sK0 + wave * M::TILE);
+      tv.store(sV0 + wave * M::TILE);
+      put_keys(t0, 0);
+      lds_barrier();
+      if (t + 1 < jb.steps) load(t0 + step);
+      blocks(sK0, sV0, 0, t0);
     }
   }
-  dsum += __shfl_xor(dsum, 32);
+  // with a fixed reference P = 2^x 2^(ref - LSE log2 e), the second factor taken here
+  const float pm = ref.fixed ? exp2_fast(ref.ref + mlse) : 1.0f;
+  dmax *= pm;
+  dsum = (dsum + __shfl_xor(dsum, 32)) * pm;
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) dmax = fmaxf(dmax, __shfl_xor(dmax, o));
   float2* dm = a.dmax + ((int64_t)h * a.njobs + pl.job) * kPackWaves + wave;
   if (jb.combine) {
-    float* stat = reinterpret_cast<float*>(sBuf + NA * 16 * 64 * 4 * 2) + lane;
+    float* stat = reinterpret_cast<float*>(sBuf0 + NA * 16 * 64 * 4 * 2) + lane;
     pack_combine(
-        reinterpret_cast<float*>(sBuf), lw, grp, gw, acc, [&](int slot) { stat[slot * 64] = dsum; },
+        reinterpret_cast<float*>(sBuf0), lw, grp, gw, acc, [&](int slot) { stat[slot * 64] = dsum; },
         [&](int slot, float& wa, float& wo) {
           dsum += stat[slot * 64];
           wa = wo = 1.0f;
         });
+    if constexpr (FIX)
+      pack_combine(reinterpret_cast<float*>(sBuf0), lw, grp, gw, fix, [](int) {},
+                   [](int, float& wa, float& wo) { wa = wo = 1.0f; });
     if (grp != 0) {
-      if (lane == 0) *dm = make_float2(dmax, 0.0f);
+      if (lane == 0) *dm = make_float2(dmax * rp, 0.0f);
       return;
     }
   }
   float cmax = fabsf(dsum);
 #pragma unroll
   for (int o = 16; o >= 1; o >>= 1) cmax = fmaxf(cmax, __shfl_xor(cmax, o));
-  if (lane == 0) *dm = make_float2(dmax, cmax);
+  if (lane == 0) *dm = make_float2(dmax * rp, cmax * rp);
   if (!iok) return;
-  const float mul = a.scale * (CAP ? M::kSlope : 1.0f);
+  const float mul = a.scale * rp * pm * (CAP ? M::kSlope : 1.0f);
+  if constexpr (FIX) {
+#pragma unroll
+    for (int c = 0; c < NA; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[c][r] = fmaf(-dsum, fix[c][r], acc[c][r]);
+  }
   T* out = rows_at<T>(a.dq, h, gr.q0 + i);
   M::features(acc, [&](int f, float4 v) {
     M::store4(out + f, make_float4(v.x * mul, v.y * mul, v.z * mul, v.w * mul));
   });
-  if (g == 0) a.dlt[h * a.ld_dlt + gr.q0 + i] = dlt + dsum;
+  if (g == 0) a.dlt[h * a.ld_dlt + gr.q0 + i] = dlt + dsum;      // D (1 - p)
 }
 
 template <class M>

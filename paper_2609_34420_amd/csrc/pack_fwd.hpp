@@ -3,11 +3,11 @@
 // Query-stationary: a wave has 32 queries and computes S^T = K Q^T, so a lane
 // owns one query and 16 keys of a 32-key block; the softmax is lane-local but
 // for the two lane halves, and O^T += V^T P^T takes P from registers. One pass
-// over the keys with a running reference m and sum l. The reference moves only
-// when needed: while every lane's block sum stays at or below 256 the block is
-// accepted as is (m is always a score the row attained, so the final sum is at
-// least 1); else the block's maximum becomes the reference and the state is
-// rescaled.
+// over the keys. Capped bf16 scores take a fixed reference where their range
+// allows it (ScoreRef); the others a running reference m, which moves only when
+// needed: while every lane's block sum stays at or below 256 the block is accepted
+// as is (m is always a score the row attained, so the final sum is at least 1);
+// else the block's maximum becomes the reference and the state is rescaled.
 //
 // P is summed in fp32 before it is rounded to bf16 for P V, so that the
 // log-sum-exp is exact to fp32; dropped pairs stay in the sum.
@@ -22,24 +22,34 @@ template <class M, bool CAP, bool DROP>
 __global__ __launch_bounds__(kPackThreads, 2) void pack_fwd_kernel(PackArgs a) {
   using T = typename M::T;
   constexpr int NA = M::NA;
+  constexpr int NB = M::BF16 && M::D == 32 ? 2 : 1;              // staged tiles
   constexpr int XCH = NA * 16 * 64 * 4 * 2 + 2 * 64 * 8;         // bytes of two waves' state
   constexpr int STG = 2 * kPackWaves * M::TILE * (int)sizeof(T);
-  __shared__ alignas(128) uint8_t sBuf[STG > XCH ? STG : XCH];
+  __shared__ alignas(128) uint8_t sBuf0[STG > XCH ? STG : XCH];
+  __shared__ alignas(128) uint8_t sBuf1[NB == 2 ? STG : 16];
   __shared__ float sTab[256];
-  T* sK = reinterpret_cast<T*>(sBuf);
-  T* sV = sK + kPackWaves * M::TILE;
+  __shared__ uint4 sKeys[DROP ? NB * kPackWaves * 4 : 1];        // KeyDraws of the staged keys
 
   const PackPlace pl(a);
   if (pl.job >= a.njobs) return;
   const int h = pl.h;
-  const PackJob jb = a.jobs[pl.job];
+  const PackJob jb = scalar_record(a.jobs + pl.job);
   const int wave = wave_id(), lane = threadIdx.x & 63, col = lane & 31, g = lane >> 5;
   const int lw = jb.log2w, W = 1 << lw;
   const int grp = wave >> lw, gw = wave & (W - 1);
-  const PackGroup gr = a.groups[jb.group + grp];
+  const PackGroup gr = scalar_record(a.groups + jb.group + grp);
+  constexpr bool START = M::BF16 && !CAP;              // the score accumulator starts from the bias
+  ScoreRef fix{false, 0.0f};
   {
     const int b = threadIdx.x;
-    sTab[b] = M::entry(b < a.n_buckets ? a.table[(int64_t)h * a.n_buckets + b] : 0.0f, a, CAP);
+    float e = M::entry(b < a.n_buckets ? a.table[(int64_t)h * a.n_buckets + b] : 0.0f, a, START);
+    if constexpr (M::BF16 && CAP) {
+      const float cap2 = a.cap * kLog2e;
+      fix = score_ref(e, cap2, reinterpret_cast<float*>(sBuf0));
+      e += cap2 - fix.ref;
+      __syncthreads();
+    }
+    sTab[b] = e;
   }
 
   const int off = gr.nk - gr.nq;
@@ -60,7 +70,10 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_fwd_kernel(PackArgs a) {
   typename M::Operand q;
   M::load_operand(rows_at<const T>(a.q, h, gr.q0 + ic), active, M::operand_mul(a, CAP), q);
   const ScoreConst sc = M::consts(a, CAP);
-  const uint32_t roff = DROP ? a.offset + (a.offset_dev ? *a.offset_dev : 0u) : 0u;
+  const Philox rng(a, h);
+  RowDraw rrow{};
+  if constexpr (DROP) rrow = rng.row((uint32_t)(gr.q0 + i));
+  const uint32_t below = (uint32_t)((a.thr - 1) & 0xffff) * 0x10001u;
 
   const PackSpdRow spd(a.spd + gr.spd + (int64_t)(active ? iw : 0) * gr.ld, gr.ld, active ? gr.nq - iw : 1,
                        active ? gr.nk : 0);
@@ -68,92 +81,160 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_fwd_kernel(PackArgs a) {
 #pragma unroll
   for (int c = 0; c < NA; ++c) acc[c] = zero_f32x16();
   float m = -INFINITY, mneg = 0.0f, l = 0.0f;
-
-  PackStage<M> tk, tv;
   uint32_t w[5];
   const int step = 32 << lw;
-  int t0 = gr.c0;                                      // the tile's first key
-  if (jb.steps > 0) {
-    tk.load(kh, a.k.rs, t0 + gw * 32, gr.nk);
-    tv.load(vh, a.v.rs, t0 + gw * 32, gr.nk);
-    spd.fetch(t0, w);
-  }
-  for (int t = 0; t < jb.steps; ++t, t0 += step) {
-    lds_barrier();                                     // the last tile's reads are done
-    tk.store(sK + wave * M::TILE);
-    tv.store(sV + wave * M::TILE);
-    lds_barrier();
-    if (t + 1 < jb.steps) {
-      tk.load(kh, a.k.rs, t0 + step + gw * 32, gr.nk);
-      tv.load(vh, a.v.rs, t0 + step + gw * 32, gr.nk);
+
+  // One 32-key block from key j0 on, staged in kt and vt.
+  auto block = [&](const T* kt, const T* vt, const uint4* keys, int j0) {
+    align_spd5(w, spd.sh);
+    float x[16], slope[16];
+    bias16(sTab, w, x);
+    spd.fetch(j0 + 32, w);                             // (past the graph it reads zeros)
+    f32x16 s = zero_f32x16();
+    if constexpr (START) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = x[r];
     }
-    for (int kb = 0; kb < W; ++kb) {
-      const int j0 = t0 + kb * 32;
-      if (j0 >= lim1) break;                           // no visible key from here on (wave-uniform)
-      const T* kt = sK + ((grp << lw) + kb) * M::TILE;
-      const T* vt = sV + ((grp << lw) + kb) * M::TILE;
-      align_spd5(w, spd.sh);
-      float x[16];
-      bias16(sTab, w, x);
-      spd.fetch(j0 + 32, w);                           // (past the graph it reads zeros)
-      f32x16 s = zero_f32x16();
-      M::rows(kt, q, s);
-      float slope;
+    M::rows(kt, q, s);
+    if constexpr (START) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) x[r] = M::template score<CAP>(s[r], x[r], sc, slope);
-      if (j0 + 32 > lim0) {
-        const int rem = lim - j0 - 16 * g;
+      for (int r = 0; r < 16; ++r) x[r] = fmaf(s[r], sc.mul, mneg);
+    } else {
+      M::template scores<CAP, false>(s, x, slope, sc);
+      if (!fix.fixed) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) x[r] = r < rem ? x[r] : -INFINITY;
+        for (int r = 0; r < 16; ++r) x[r] += mneg;
       }
-      float p[16];
-      float bs = 0.0f;
+    }
+    if (j0 + 32 > lim0) keep_below(x, lim - j0 - 16 * g, -INFINITY);
+    float p[16];
+    float bs = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      p[r] = M::expo(x[r]);
+      bs += p[r];
+    }
+    if (!fix.fixed && __any(!(bs <= 256.0f) || m == -INFINITY)) {    // move the reference to the block's maximum
+      float mx = x[0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) mx = fmaxf(mx, x[r]);
+      mx = fmaxf(mx, __shfl_xor(mx, 32)) - mneg;
+      const float mn = fmaxf(m, mx);
+      const float alpha = m == -INFINITY ? 0.0f : M::expo(m - mn);
+      l *= alpha;
+#pragma unroll
+      for (int c = 0; c < NA; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[c][r] *= alpha;
+      m = mn;
+      const float shift = (mn == -INFINITY ? 0.0f : -mn) - mneg;
+      mneg += shift;
+      bs = 0.0f;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        p[r] = M::expo(x[r], mneg);
+        p[r] = M::expo(x[r] + shift);
         bs += p[r];
       }
-      if (__any(!(bs <= 256.0f) || m == -INFINITY)) {  // move the reference to the block's maximum
-        float mx = x[0];
-#pragma unroll
-        for (int r = 1; r < 16; ++r) mx = fmaxf(mx, x[r]);
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
-        const float mn = fmaxf(m, mx);
-        const float alpha = m == -INFINITY ? 0.0f : M::expo(m, -mn);
-        l *= alpha;
-#pragma unroll
-        for (int c = 0; c < NA; ++c)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) acc[c][r] *= alpha;
-        m = mn;
-        mneg = mn == -INFINITY ? 0.0f : -mn;
-        bs = 0.0f;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          p[r] = M::expo(x[r], mneg);
-          bs += p[r];
-        }
-      }
-      l += bs;
-      if constexpr (DROP) {
-        uint32_t rw[8];
-        draw16(a, roff, h, (uint32_t)(gr.q0 + i), j0 + 16 * g, rw);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) p[r] = kept(rw, r, a.thr) ? p[r] : 0.0f;
-      }
+    }
+    l += bs;
+    if constexpr (DROP) {
+      uint32_t rw[8];
+      rng.draw(rrow, keys[2 * g], rw);
+      rng.draw(rrow, keys[2 * g + 1], rw + 4);
+      M::cols_kept(vt, p, rw, below, a.thr, acc);
+    } else {
       M::cols(vt, p, acc);
+    }
+  };
+  // The wave's part of the tile from key t0 on: KeyDraws of its 32 staged keys.
+  auto put_keys = [&](int t0, int buf) {
+    if constexpr (DROP) {
+      const uint4 k = rng.keys((uint32_t)(t0 + gw * 32) / 8u + (uint32_t)(lane & 3));
+      if (lane < 4) sKeys[(buf * kPackWaves + wave) * 4 + lane] = k;
+    }
+  };
+  auto blocks = [&](const T* sK, const T* sV, int buf, int t0) {
+    for (int kb = 0; kb < W; ++kb) {
+      const int j0 = t0 + kb * 32, slot = (grp << lw) + kb;
+      if (j0 >= lim1) break;                           // no visible key from here on (wave-uniform)
+      block(sK + slot * M::TILE, sV + slot * M::TILE, sKeys + (DROP ? (buf * kPackWaves + slot) * 4 : 0), j0);
+    }
+  };
+
+  int t0 = gr.c0;                                      // the tile's first key
+  T* const sK0 = reinterpret_cast<T*>(sBuf0);
+  T* const sV0 = sK0 + kPackWaves * M::TILE;
+  if (jb.steps > 0) spd.fetch(t0, w);
+  if constexpr (M::BF16) {
+    const PackDma<M> dk(a.k.rs), dv(a.v.rs);
+    auto copy = [&](T* k, T* v, int t) {
+      dk.load(kh, a.k.rs, t + gw * 32, gr.nk, k + wave * M::TILE);
+      dv.load(vh, a.v.rs, t + gw * 32, gr.nk, v + wave * M::TILE);
+    };
+    if constexpr (NB == 1) {
+      for (int t = 0; t < jb.steps; ++t, t0 += step) {
+        lds_barrier();                                 // the last tile's reads are done
+        copy(sK0, sV0, t0);
+        put_keys(t0, 0);
+        wait_vmcnt<0>();
+        lds_barrier();                                 // the tile has landed
+        blocks(sK0, sV0, 0, t0);
+      }
+      t0 = 0;
+    }
+    T* const sK1 = reinterpret_cast<T*>(sBuf1);
+    T* const sV1 = sK1 + (NB == 2 ? kPackWaves * M::TILE : 0);
+    if (NB == 2 && jb.steps > 0) {
+      copy(sK0, sV0, t0);
+      put_keys(t0, 0);
+    }
+    for (int t = 0; NB == 2 && t < jb.steps; t += 2) {
+      wait_vmcnt<0>();
+      lds_barrier();                                   // the tile has landed, the last one's reads are done
+      if (t + 1 < jb.steps) {
+        copy(sK1, sV1, t0 + step);
+        put_keys(t0 + step, 1);
+      }
+      blocks(sK0, sV0, 0, t0);
+      t0 += step;
+      if (t + 1 >= jb.steps) break;
+      wait_vmcnt<0>();
+      lds_barrier();
+      if (t + 2 < jb.steps) {
+        copy(sK0, sV0, t0 + step);
+        put_keys(t0 + step, 0);
+      }
+      blocks(sK1, sV1, 1, t0);
+      t0 += step;
+    }
+  } else {
+    PackStage<M> tk, tv;
+    auto load = [&](int t) {
+      tk.load(kh, a.k.rs, t + gw * 32, gr.nk);
+      tv.load(vh, a.v.rs, t + gw * 32, gr.nk);
+    };
+    if (jb.steps > 0) load(t0);
+    for (int t = 0; t < jb.steps; ++t, t0 += step) {
+      lds_barrier();                                   // the last tile's reads are done
+      tk.store(sK0 + wave * M::TILE);
+      tv.store(sV0 + wave * M::TILE);
+      put_keys(t0, 0);
+      lds_barrier();
+      if (t + 1 < jb.steps) load(t0 + step);
+      blocks(sK0, sV0, 0, t0);
     }
   }
   l += __shfl_xor(l, 32);
+  if (fix.fixed) m = l == 0.0f ? -INFINITY : fix.ref;
   if (jb.combine) {
-    float2* stat = reinterpret_cast<float2*>(sBuf + NA * 16 * 64 * 4 * 2) + lane;
+    float2* stat = reinterpret_cast<float2*>(sBuf0 + NA * 16 * 64 * 4 * 2) + lane;
     pack_combine(
-        reinterpret_cast<float*>(sBuf), lw, grp, gw, acc, [&](int slot) { stat[slot * 64] = make_float2(m, l); },
+        reinterpret_cast<float*>(sBuf0), lw, grp, gw, acc, [&](int slot) { stat[slot * 64] = make_float2(m, l); },
         [&](int slot, float& wa, float& wo) {
           const float2 o = stat[slot * 64];
           const float mn = fmaxf(m, o.x);
-          wa = m == -INFINITY ? 0.0f : M::expo(m, -mn);
-          wo = o.x == -INFINITY ? 0.0f : M::expo(o.x, -mn);
+          wa = m == -INFINITY ? 0.0f : M::expo(m - mn);
+          wo = o.x == -INFINITY ? 0.0f : M::expo(o.x - mn);
           l = fmaf(l, wa, o.y * wo);
           m = mn;
         });

@@ -50,7 +50,7 @@ def upload(a):
     return r
 
 
-def compare(tag, dt, got, want, total=None):
+def compare(tag, dt, got, want, f32=None):
     names = ("O", "LSE", "dQ", "dK", "dV", "dtable")
     for name, x, y in zip(names, got, want):
         x = to_np(x)
@@ -59,6 +59,8 @@ def compare(tag, dt, got, want, total=None):
         assert np.isfinite(x[fin]).all(), (tag, name, "non-finite")
         e = rel_l2(x[fin], y[fin])
         lim = TOL[dt]["f32" if name in ("LSE", "dtable") else ("o" if name == "O" else "grad")]
+        if f32 is not None and (dt == "f32" or name in ("LSE", "dtable")):
+            lim = f32
         say(f"{tag}: {name} {e:.2e} (limit {lim:.1e})")
         assert e <= lim, (tag, name, e)
 
@@ -165,6 +167,36 @@ def test_masked_entries_and_empty_rows(dt):
         for row in (7, 77):
             assert bool((o[:, row] == 0).all()) and bool(torch.isneginf(lse[:, row]).all())
             assert bool((grads[0][:, row] == 0).all())
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("cap,spread", [(200.0, 0.0), (30.0, 60.0), (30.0, 5.0), (1e6, 0.0), (0.01, 0.0)])
+def test_ranges_of_capped_scores(dt, cap, spread):
+    """Caps and biases whose scores span more than a fixed reference allows, and
+    less; biases of rows that differ by the spread. fp32 outputs: a cap of 200
+    makes terms of up to 2 cap log2 e = 577 of the score, 577 (2^-23 + 2^-24) ln 2 = 7.2e-5,
+    twice that. At a cap of 0.01 the slope 1 - tanh^2(u / cap) takes up u's rounding:
+    a sum of 32 products of up to 10, times 0.18, is off by up to 32 * 10 * 0.18 * 2^-24 =
+    3.4e-6, 3.4e-4 of the cap. One of 1e6 only cancels where tanh is near its linear part, and
+    the scores of order ten are off by cap 2^-23 = 0.12 of that sum's terms, so bf16
+    leaves that case to the finite check."""
+    n, H, d, nb = [70, 130], 2, 32, 12
+    a = make(n, n, H, d, nb, dt, seed=12, gain=2.0)
+    if spread:
+        a["table"] += (spread * (np.arange(nb) % 3 - 1)).astype(np.float32)
+    r = upload(a)
+    pack = gt.gt_attn_pack(n, H, device=DEV)
+    args = (r["q"], r["k"], r["v"], r["spd"], r["table"], pack)
+    o, lse = gt.gt_attn_pack_fwd(*args, cap=cap)
+    grads = gt.gt_attn_pack_bwd(*args, o, lse, r["do"], cap=cap)
+    torch.cuda.synchronize()
+    assert all(bool(torch.isfinite(x.float()).all()) for x in (o, lse, *grads))
+    if cap == 1e6:
+        return
+    s = d ** -0.5
+    want = (*oracle.packed_forward(a["q"], a["k"], a["v"], a["spd"], a["table"], s, n, n, cap=cap),
+            *oracle.packed_backward(a["q"], a["k"], a["v"], a["spd"], a["table"], s, a["do"], n, n, cap=cap))
+    compare(f"range {dt} cap={cap} spread={spread}", dt, (o, lse, *grads), want, f32={200.0: 1.5e-4, 0.01: 3.4e-4}.get(cap))
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
