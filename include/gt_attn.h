@@ -377,8 +377,8 @@ typedef struct {
   int64_t plan_bytes;
   int32_t n_graphs, H;
   /* internal: the kernels' work lists inside the plan */
-  int32_t jobs[3], merges, parts, reserved;
-  int64_t job_off[3], group_off[3], merge_off;
+  int32_t jobs[3], merges, parts, slots;
+  int64_t job_off[3], merge_off;
 } gt_attn_pack_t;
 
 typedef struct {

@@ -44,9 +44,10 @@ struct PackArgs {
   float rp;                 // 1 / (1 - p)
   uint32_t seed0, seed1, offset;
   const uint32_t* offset_dev;   // added to offset, or null
-  const PackJob* jobs;
-  const PackGroup* groups;
+  const PackWave* jobs;     // 4 per job
   int32_t njobs;
+  int32_t slots;            // key-stationary: workgroups per head
+  int32_t hist;             // and buckets of its histogram, a power of two above n_buckets (256 at most)
   const PackMerge* merges;
   int32_t nmerges;
   float* o_part;            // [slot, H, 32, d]
@@ -56,7 +57,7 @@ struct PackArgs {
   float2* dmax;             // [H, njobs_dq * 4] of each wave of the dQ kernel: largest |dS|, and
                             // largest correction of a row's D
   int32_t njobs_dq;
-  double* dtab_part;        // [H, njobs, n_buckets]
+  double* dtab_part;        // [H, slots, n_buckets]
   float* dtable;            // [H, n_buckets]
 };
 
@@ -474,18 +475,18 @@ struct PackDma {
   }
 };
 
-// The workgroup's job and head, the wave's group. Workgroups go to the 8 XCDs
+// The workgroup's job and head, of `jobs` and a.H. Workgroups go to the 8 XCDs
 // round robin: with many jobs, a job's heads, which share its distances, stay on
 // one XCD, and the jobs, longest first, are dealt over the XCDs in turn.
 constexpr int kXcdJobs = 64;
-__host__ __device__ inline unsigned pack_grid(int njobs, int H) {
-  return njobs >= kXcdJobs ? (unsigned)((njobs + 7) / 8 * 8) * (unsigned)H : (unsigned)njobs * (unsigned)H;
+__host__ __device__ inline unsigned pack_grid(int jobs, int H) {
+  return jobs >= kXcdJobs ? (unsigned)((jobs + 7) / 8 * 8) * (unsigned)H : (unsigned)jobs * (unsigned)H;
 }
 struct PackPlace {
   int job, h;
-  __device__ __forceinline__ explicit PackPlace(const PackArgs& a) {
+  __device__ __forceinline__ PackPlace(const PackArgs& a, int jobs) {
     const int w = (int)blockIdx.x;
-    if (a.njobs >= kXcdJobs) {
+    if (jobs >= kXcdJobs) {
       const int i = w >> 3;
       h = i % a.H;
       job = i / a.H * 8 + (w & 7);

@@ -16,8 +16,8 @@ inline bool aligned(const void* p, unsigned n) { return reinterpret_cast<uintptr
 bool pack_ok(const gt_attn_pack_t* p) {
   if (!p || p->H < 1 || p->n_graphs < 1 || p->total_q < 0 || p->total_k < 0 || p->spd_bytes < 0) return false;
   for (int i = 0; i < 3; ++i)
-    if (p->jobs[i] < 0 || p->job_off[i] < 0 || p->group_off[i] < 0) return false;
-  return p->merges >= 0 && p->parts >= 0 && p->merge_off >= 0;
+    if (p->jobs[i] < 0 || p->job_off[i] < 0) return false;
+  return p->merges >= 0 && p->parts >= 0 && p->merge_off >= 0 && p->slots >= 0 && p->slots <= p->jobs[2];
 }
 
 bool rows_ok(const gt_attn_rows_t* t, int64_t rows, int32_t d, gt_dtype_t dtype) {
@@ -77,9 +77,7 @@ gt_status_t common(const gt_attn_pack_t* pack, const void* plan, const gt_attn_r
 
 // The work list of stage i (0 forward, 1 dQ, 2 dK / dV).
 void stage(const gt_attn_pack_t* pack, const void* plan, int i, PackArgs& a) {
-  const uint8_t* p = static_cast<const uint8_t*>(plan);
-  a.jobs = reinterpret_cast<const PackJob*>(p + pack->job_off[i]);
-  a.groups = reinterpret_cast<const PackGroup*>(p + pack->group_off[i]);
+  a.jobs = reinterpret_cast<const PackWave*>(static_cast<const uint8_t*>(plan) + pack->job_off[i]);
   a.njobs = pack->jobs[i];
 }
 
@@ -95,7 +93,7 @@ BwdParts bwd_parts(const gt_attn_pack_t* p, int32_t n_buckets) {
   BwdParts b;
   b.dmax = pad256(H * (size_t)p->total_q * sizeof(float));
   b.dtab = b.dmax + pad256(H * (size_t)p->jobs[1] * kPackWaves * sizeof(float2));
-  b.bytes = b.dtab + pad256(H * (size_t)p->jobs[2] * (size_t)n_buckets * sizeof(double));
+  b.bytes = b.dtab + pad256(H * (size_t)p->slots * (size_t)n_buckets * sizeof(double));
   return b;
 }
 
@@ -165,6 +163,7 @@ gt_status_t gt_attn_pack_bwd(const gt_attn_pack_t* pack, const void* plan, const
   a.d_o = gt::tensor(d_o); a.dq = gt::tensor(dq); a.dk = gt::tensor(dk); a.dv = gt::tensor(dv);
   a.dtable = dtable;
   a.njobs_dq = pack->jobs[1];
+  a.slots = pack->slots;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const bool bf16 = dtype == GT_BF16, c = cap > 0.0f, drop = a.thr > -32768;
   hipError_t e = hipSuccess;

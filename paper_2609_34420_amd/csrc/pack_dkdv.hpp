@@ -13,7 +13,7 @@
 //
 // Table gradient: dS is added into an LDS histogram in fixed point, 64-bit sums of
 // round(dS 2^F) (float adds to LDS are some twenty times slower), in 32 copies
-// (lane & 31) of up to 128 buckets or 16 of 256. F comes from the largest
+// (lane & 31) of 32, 64 or 128 buckets or 16 of 256. F comes from the largest
 // |dS| that the dQ kernel met in this head, so that every term stays below 2^31
 // and the rounding of 2^-31 of it is far below the sums in fp32; V's operand and
 // the staged D carry it, so that dS arrives scaled. Each workgroup writes its
@@ -25,8 +25,6 @@
 namespace gt {
 
 namespace {
-
-constexpr int kPackHist = 4096;
 
 __device__ __forceinline__ int pack_round(float x) {
   int r;
@@ -49,10 +47,10 @@ __device__ __forceinline__ void transpose_bytes(uint8_t* st, int at, uint4 v, co
   }
 }
 
-// WIDE: more than 127 buckets (the narrow layout keeps bucket 127 for the bytes
+// WIDE: more than 127 buckets (a narrow layout keeps its last bucket for the bytes
 // past it).
 template <class M, bool CAP, bool DROP, bool WIDE>
-__global__ __launch_bounds__(kPackThreads, 2) void pack_dkdv_kernel(PackArgs a) {
+__global__ __launch_bounds__(kPackThreads, M::D == 32 && M::BF16 ? 2 : (M::BF16 || M::D < 64 ? 2 : 1)) void pack_dkdv_kernel(PackArgs a) {
   using T = typename M::T;
   constexpr int NA = M::NA;
   // staged tiles: two where both fit beside the histogram twice per compute unit
@@ -60,10 +58,10 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_dkdv_kernel(PackArgs a) 
   constexpr int XCH = NA * 16 * 64 * 4 * 2;
   constexpr int STG = 2 * kPackWaves * M::TILE * (int)sizeof(T);
   constexpr int CPY = WIDE ? 16 : 32;
-  // (LDS objects are placed by decreasing alignment: the table and the histogram
-  // first, where a DS immediate of 16 bits reaches them)
+  // (LDS objects are placed by decreasing alignment: the table first, where a DS
+  // immediate of 16 bits reaches it)
+  extern __shared__ unsigned long long hist[];            // a.hist buckets of CPY copies
   __shared__ alignas(4096) float sTab[256];
-  __shared__ alignas(2048) unsigned long long hist[kPackHist];
   __shared__ alignas(1024) uint8_t sByte[kPackWaves][1024];
   __shared__ alignas(512) float sStat[NB][kPackWaves][64]; // per staged row: -LSE; D (1 - p) 2^F, negative without dropout
   __shared__ alignas(128) uint8_t sBuf0[STG > XCH ? STG : XCH];
@@ -71,18 +69,14 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_dkdv_kernel(PackArgs a) 
   __shared__ float red[2][kPackWaves];
   __shared__ int bad[kPackWaves];
 
-  const PackPlace pl(a);
-  if (pl.job >= a.njobs) return;
+  const PackPlace pl(a, a.slots);
+  if (pl.job >= a.slots) return;
   const int h = pl.h;
-  const PackJob jb = scalar_record(a.jobs + pl.job);
   const int tid = threadIdx.x, wave = wave_id(), lane = tid & 63, col = lane & 31, g = lane >> 5;
-  const int lw = jb.log2w, W = 1 << lw;
-  const int grp = wave >> lw, gw = wave & (W - 1);
-  const PackGroup gr = scalar_record(a.groups + jb.group + grp);
   sTab[tid] = M::entry(tid < a.n_buckets ? a.table[(int64_t)h * a.n_buckets + tid] : 0.0f, a, false)
               + (M::BF16 && CAP ? a.cap * kLog2e : 0.0f);
-  for (int t = tid; t < kPackHist / 2; t += kPackThreads)
-    if (t < a.n_buckets * CPY / 2) reinterpret_cast<uint4*>(hist)[t] = make_uint4(0u, 0u, 0u, 0u);
+  for (int t = tid; t < a.n_buckets * CPY / 2; t += kPackThreads)
+    reinterpret_cast<uint4*>(hist)[t] = make_uint4(0u, 0u, 0u, 0u);
   {
     const float2* dm = a.dmax + (int64_t)h * a.njobs_dq * kPackWaves;
     float x = 0.0f, y = 0.0f;
@@ -119,256 +113,264 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_dkdv_kernel(PackArgs a) 
   }
   const float sF = ldexpf(1.0f, fexp);
 
-  const int off = gr.nk - gr.nq;
-  const int jw = gr.row0 + gw * 32;                       // the wave's first key
-  const int j = jw + col;
-  const bool active = jw < gr.nk;
-  const bool jok = j < gr.nk;
-  const int jc = jok ? j : (active ? gr.nk - 1 : 0);
-  // queries from the bound on see the key: the lane's, the wave's least and most
-  const int jl = jw + 31 < gr.nk ? jw + 31 : gr.nk - 1;
-  auto first = [&](int key) { return key < gr.prefix ? 0 : key - off; };
-  const int lo = first(jc), lo0 = first(jw), lo1 = first(jl);
-  const T* qh = rows_at<const T>(a.q, h, gr.q0);
-  const T* oh = rows_at<const T>(a.d_o, h, gr.q0);
-  const float* lseh = a.lse + h * a.ld_lse + gr.q0;
-  const float* dlth = a.dlt + h * a.ld_dlt + gr.q0;
-  typename M::Operand k, v;
-  M::load_operand(rows_at<const T>(a.k, h, gr.k0 + jc), active, M::operand_mul(a, CAP), k);
-  M::load_operand(rows_at<const T>(a.v, h, gr.k0 + jc), active, sF, v);
   const ScoreConst sc = M::consts(a, CAP);
   // uncapped bf16: the score accumulator starts from -LSE log2 e / mul
   constexpr bool START = M::BF16 && !CAP;
   const float ml_mul = START ? 1.0f / sc.mul : 1.0f;
   const float d_mul = DROP ? sF : -sF;
   const Philox rng(a, h);
-  uint4 rk0{}, rk1{};
-  if constexpr (DROP) {
-    rk0 = rng.keys((uint32_t)(jw + 16 * g) / 8u);
-    rk1 = rng.keys((uint32_t)(jw + 16 * g) / 8u + 1u);
-  }
   const uint32_t below = (uint32_t)((a.thr - 1) & 0xffff) * 0x10001u;
-
-  f32x16 dk[NA], dv[NA];
-#pragma unroll
-  for (int c = 0; c < NA; ++c) {
-    dk[c] = zero_f32x16();
-    dv[c] = zero_f32x16();
-  }
-
-  // spd bytes of a block: lane l loads 16 bytes of query row l / 2, from key
-  // 16 (l & 1) of the wave's on, which are transposed through LDS. A block's first
-  // row is a multiple of 32, so the lane's address mod 4 stays the same.
-  const uint8_t* sbase = a.spd + gr.spd + (active ? jw : 0);
-  const uint32_t srem = (uint32_t)(reinterpret_cast<uintptr_t>(sbase) & 15u);
-  uint32_t svoff = (uint32_t)((lane >> 1) * (int64_t)gr.ld) + 16u * (uint32_t)(lane & 1) + srem;
-  const uint32_t ssh = svoff & 3u;
-  svoff -= ssh;
-  auto fetch = [&](int i0, uint32_t (&w)[5]) {
-    const int64_t n = gr.nq - i0 < 32 ? gr.nq - i0 : 32;
-    const int64_t bytes = n > 0 && active ? (n - 1) * (int64_t)gr.ld + (gr.nk - jw) + srem + 3 : 0;
-    load_spd5(make_rsrc_n(sbase - srem + (n > 0 ? (int64_t)i0 * gr.ld : 0), bytes & ~(int64_t)3), svoff, w);
-  };
   int off_tr8[2];
 #pragma unroll
   for (int hh = 0; hh < 2; ++hh)
     off_tr8[hh] = (16 * g + 8 * hh + ((lane & 15) >> 1)) * 32 + 16 * ((lane >> 4) & 1) + 8 * (lane & 1);
 
-  uint32_t w[5];
-  const int step = 32 << lw;
-  float stat = 0.0f;
-  auto load_stat = [&](int i0) {
-    const int r = i0 + col < gr.nq ? i0 + col : gr.nq - 1;
-    if (gr.nq > 0) stat = (g == 0 ? lseh : dlth)[r];
-  };
-  auto store_stat = [&](int i0, int buf) {
-    float x = stat;
-    opaque_f(x);
-    const bool in = i0 + col < gr.nq;
-    if (g == 0)
-      x = in && x != -INFINITY ? -M::to_unit(x) * ml_mul : -INFINITY;
-    else
-      x = in ? x * d_mul : 0.0f;
-    sStat[buf][wave][lane] = x;
-  };
+  const float rp = DROP ? a.rp : 1.0f;
+  const float mk = a.scale * rp * ldexpf(1.0f, -fexp) * (CAP ? M::kSlope : 1.0f);
+  bool any_bad = false;
 
-  // One block of 32 queries from i0 on, staged in qt and ot.
-  auto block = [&](const T* qt, const T* ot, const float* st, int i0) {
-    align_spd5(w, ssh);
-    const uint4 w4 = make_uint4(w[0], w[1], w[2], w[3]);
-    fetch(i0 + 32, w);
-    if (i0 + 31 < lo0) return;                            // no query of the block sees a key (wave-uniform)
-    uint32_t b[4];
-    transpose_bytes(sByte[wave], 16 * lane, w4, off_tr8, b);
-    f32x16 s, dp;
-    float x[16], slope[16], ml[16], dl[16];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const float4 y = *reinterpret_cast<const float4*>(st + 16 * g + 4 * u);
-      const float4 z = *reinterpret_cast<const float4*>(st + 32 + 16 * g + 4 * u);
-      ml[4 * u] = y.x; ml[4 * u + 1] = y.y; ml[4 * u + 2] = y.z; ml[4 * u + 3] = y.w;
-      dl[4 * u] = z.x; dl[4 * u + 1] = z.y; dl[4 * u + 2] = z.z; dl[4 * u + 3] = z.w;
-    }
-    bias16(sTab, b, x);
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      s[r] = START ? ml[r] : 0.0f;
-      dp[r] = DROP ? 0.0f : dl[r];
-    }
-    M::rows(qt, k, s);
-    M::rows(ot, v, dp);
-    if constexpr (START) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) x[r] = fmaf(s[r], sc.mul, x[r]);
-    } else {
-      M::template scores<CAP, true>(s, x, slope, sc);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) x[r] += ml[r];
-    }
-    float p[16];
-#pragma unroll
-    for (int r = 0; r < 16; ++r) p[r] = M::expo(x[r]);
-    if (i0 < lo1 || jw + 32 > gr.nk) {
-      const int r0 = jok ? lo - i0 - 16 * g : 16;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) p[r] = r >= r0 ? p[r] : 0.0f;
-    }
+  for (int job = pl.job; job < a.njobs; job += a.slots) {
+    const PackWave gr = scalar_record(a.jobs + (int64_t)job * kPackWaves + wave);
+    const int lw = gr.log2w, W = 1 << lw;
+    const int grp = wave >> lw, gw = wave & (W - 1);
+    const int off = gr.nk - gr.nq;
+    const int jw = gr.row;                       // the wave's first key
+    const int j = jw + col;
+    const bool active = jw < gr.nk;
+    const bool jok = j < gr.nk;
+    const int jc = jok ? j : (active ? gr.nk - 1 : 0);
+    // queries from the bound on see the key: the lane's, the wave's least and most
+    const int jl = jw + 31 < gr.nk ? jw + 31 : gr.nk - 1;
+    auto first = [&](int key) { return key < gr.prefix ? 0 : key - off; };
+    const int lo = first(jc), lo0 = first(jw), lo1 = first(jl);
+    const T* qh = rows_at<const T>(a.q, h, gr.q0);
+    const T* oh = rows_at<const T>(a.d_o, h, gr.q0);
+    const float* lseh = a.lse + h * a.ld_lse + gr.q0;
+    const float* dlth = a.dlt + h * a.ld_dlt + gr.q0;
+    typename M::Operand k, v;
+    M::load_operand(rows_at<const T>(a.k, h, gr.k0 + jc), active, M::operand_mul(a, CAP), k);
+    M::load_operand(rows_at<const T>(a.v, h, gr.k0 + jc), active, sF, v);
+    uint4 rk0{}, rk1{};
     if constexpr (DROP) {
-      uint32_t rw[8], z[4];
-      const RowDraw rr = rng.row((uint32_t)(gr.q0 + i0 + col));
-      rng.draw(rr, rk0, rw);
-      rng.draw(rr, rk1, rw + 4);
-      uint4 kb;
-      kb.x = __builtin_amdgcn_perm(kept2(rw[1], below), kept2(rw[0], below), 0x06040200u) & 0x01010101u;
-      kb.y = __builtin_amdgcn_perm(kept2(rw[3], below), kept2(rw[2], below), 0x06040200u) & 0x01010101u;
-      kb.z = __builtin_amdgcn_perm(kept2(rw[5], below), kept2(rw[4], below), 0x06040200u) & 0x01010101u;
-      kb.w = __builtin_amdgcn_perm(kept2(rw[7], below), kept2(rw[6], below), 0x06040200u) & 0x01010101u;
-      transpose_bytes(sByte[wave], 32 * col + 16 * g, kb, off_tr8, z);
+      rk0 = rng.keys((uint32_t)(jw + 16 * g) / 8u);
+      rk1 = rng.keys((uint32_t)(jw + 16 * g) / 8u + 1u);
+    }
+
+    f32x16 dk[NA], dv[NA];
+#pragma unroll
+    for (int c = 0; c < NA; ++c) {
+      dk[c] = zero_f32x16();
+      dv[c] = zero_f32x16();
+    }
+
+    // spd bytes of a block: lane l loads 16 bytes of query row l / 2, from key
+    // 16 (l & 1) of the wave's on, which are transposed through LDS. A block's first
+    // row is a multiple of 32, so the lane's address mod 4 stays the same.
+    const uint8_t* sbase = a.spd + gr.spd + (active ? jw : 0);
+    const uint32_t srem = (uint32_t)(reinterpret_cast<uintptr_t>(sbase) & 15u);
+    uint32_t svoff = (uint32_t)((lane >> 1) * (int64_t)gr.ld) + 16u * (uint32_t)(lane & 1) + srem;
+    const uint32_t ssh = svoff & 3u;
+    svoff -= ssh;
+    auto fetch = [&](int i0, uint32_t (&w)[5]) {
+      const int64_t n = gr.nq - i0 < 32 ? gr.nq - i0 : 32;
+      const int64_t bytes = n > 0 && active ? (n - 1) * (int64_t)gr.ld + (gr.nk - jw) + srem + 3 : 0;
+      load_spd5(make_rsrc_n(sbase - srem + (n > 0 ? (int64_t)i0 * gr.ld : 0), bytes & ~(int64_t)3), svoff, w);
+    };
+    uint32_t w[5];
+    const int step = 32 << lw;
+    float stat = 0.0f;
+    auto load_stat = [&](int i0) {
+      const int r = i0 + col < gr.nq ? i0 + col : gr.nq - 1;
+      if (gr.nq > 0) stat = (g == 0 ? lseh : dlth)[r];
+    };
+    auto store_stat = [&](int i0, int buf) {
+      float x = stat;
+      opaque_f(x);
+      const bool in = i0 + col < gr.nq;
+      if (g == 0)
+        x = in && x != -INFINITY ? -M::to_unit(x) * ml_mul : -INFINITY;
+      else
+        x = in ? x * d_mul : 0.0f;
+      sStat[buf][wave][lane] = x;
+    };
+
+    // One block of 32 queries from i0 on, staged in qt and ot.
+    auto block = [&](const T* qt, const T* ot, const float* st, int i0) {
+      align_spd5(w, ssh);
+      const uint4 w4 = make_uint4(w[0], w[1], w[2], w[3]);
+      fetch(i0 + 32, w);
+      if (i0 + 31 < lo0) return;                            // no query of the block sees a key (wave-uniform)
+      uint32_t b[4];
+      transpose_bytes(sByte[wave], 16 * lane, w4, off_tr8, b);
+      f32x16 s, dp;
+      float x[16], slope[16], ml[16], dl[16];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const float4 y = *reinterpret_cast<const float4*>(st + 16 * g + 4 * u);
+        const float4 z = *reinterpret_cast<const float4*>(st + 32 + 16 * g + 4 * u);
+        ml[4 * u] = y.x; ml[4 * u + 1] = y.y; ml[4 * u + 2] = y.z; ml[4 * u + 3] = y.w;
+        dl[4 * u] = z.x; dl[4 * u + 1] = z.y; dl[4 * u + 2] = z.z; dl[4 * u + 3] = z.w;
+      }
+      bias16(sTab, b, x);
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const float pz = p[r] * (float)((z[r >> 2] >> (8 * (r & 3))) & 0xffu);
-        x[r] = fmaf(pz, dp[r], -p[r] * dl[r]);
-        p[r] = pz;
+        s[r] = START ? ml[r] : 0.0f;
+        dp[r] = DROP ? 0.0f : dl[r];
       }
-    } else {
+      M::rows(qt, k, s);
+      M::rows(ot, v, dp);
+      if constexpr (START) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) x[r] = p[r] * dp[r];
-    }
-    if constexpr (!WIDE) {
-      if (__any(((b[0] | b[1] | b[2] | b[3]) & 0x80808080u) != 0)) {     // past the narrow layout: to 127
+        for (int r = 0; r < 16; ++r) x[r] = fmaf(s[r], sc.mul, x[r]);
+      } else {
+        M::template scores<CAP, true>(s, x, slope, sc);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const uint32_t hi = (b[u] >> 7) & 0x01010101u;
-          b[u] = (b[u] | hi * 0x7fu) & 0x7f7f7f7fu;
+        for (int r = 0; r < 16; ++r) x[r] += ml[r];
+      }
+      float p[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) p[r] = M::expo(x[r]);
+      if (i0 < lo1 || jw + 32 > gr.nk) {
+        const int r0 = jok ? lo - i0 - 16 * g : 16;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) p[r] = r >= r0 ? p[r] : 0.0f;
+      }
+      if constexpr (DROP) {
+        uint32_t rw[8], z[4];
+        const RowDraw rr = rng.row((uint32_t)(gr.q0 + i0 + col));
+        rng.draw(rr, rk0, rw);
+        rng.draw(rr, rk1, rw + 4);
+        uint4 kb;
+        kb.x = __builtin_amdgcn_perm(kept2(rw[1], below), kept2(rw[0], below), 0x06040200u) & 0x01010101u;
+        kb.y = __builtin_amdgcn_perm(kept2(rw[3], below), kept2(rw[2], below), 0x06040200u) & 0x01010101u;
+        kb.z = __builtin_amdgcn_perm(kept2(rw[5], below), kept2(rw[4], below), 0x06040200u) & 0x01010101u;
+        kb.w = __builtin_amdgcn_perm(kept2(rw[7], below), kept2(rw[6], below), 0x06040200u) & 0x01010101u;
+        transpose_bytes(sByte[wave], 32 * col + 16 * g, kb, off_tr8, z);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float pz = p[r] * (float)((z[r >> 2] >> (8 * (r & 3))) & 0xffu);
+          x[r] = fmaf(pz, dp[r], -p[r] * dl[r]);
+          p[r] = pz;
+        }
+      } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[r] = p[r] * dp[r];
+      }
+      if constexpr (!WIDE) {
+        // bytes past the layout go to its last bucket
+        const uint32_t past = (0x100u - (uint32_t)a.hist) * 0x01010101u;
+        if (__any(((b[0] | b[1] | b[2] | b[3]) & past) != 0)) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int e = 0; e < 32; e += 8)
+              if ((b[u] & past) >> e & 0xffu) b[u] = (b[u] & ~(0xffu << e)) | (uint32_t)(a.hist - 1) << e;
         }
       }
-    }
-    const uint32_t copy = (uint32_t)(lane & (CPY - 1)) * 8u;
+      const uint32_t copy = (uint32_t)(lane & (CPY - 1)) * 8u;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const uint32_t at = WIDE ? ((((b[r >> 2] >> (8 * (r & 3))) & 0xffu) << 7) | copy)
-                               : __builtin_amdgcn_perm(b[r >> 2], copy, 0x0c0c0000u | ((4u + (r & 3)) << 8));
-      atomicAdd(reinterpret_cast<unsigned long long*>(reinterpret_cast<uint8_t*>(hist) + at),
-                (unsigned long long)(long long)pack_round(x[r]));
-      if constexpr (CAP) x[r] *= slope[r];
-    }
-    M::cols(ot, p, dv);
-    M::cols(qt, x, dk);
-  };
-  auto blocks = [&](const T* sQ, const T* sO, int buf, int t0) {
-    if (!active) return;
-    for (int ib = 0; ib < W; ++ib) {
-      const int i0 = t0 + ib * 32, slot = (grp << lw) + ib;
-      if (i0 >= gr.c1) break;
-      block(sQ + slot * M::TILE, sO + slot * M::TILE, sStat[buf][slot], i0);
-    }
-  };
-
-  int t0 = gr.c0;
-  T* const sQ0 = reinterpret_cast<T*>(sBuf0);
-  T* const sO0 = sQ0 + kPackWaves * M::TILE;
-  if (jb.steps > 0) {
-    load_stat(t0 + gw * 32);
-    fetch(t0, w);
-  }
-  if constexpr (M::BF16) {
-    const PackDma<M> cq(a.q.rs), co(a.d_o.rs);
-    auto stage = [&](T* q, T* o, int buf, int t) {
-      cq.load(qh, a.q.rs, t + gw * 32, gr.nq, q + wave * M::TILE);
-      co.load(oh, a.d_o.rs, t + gw * 32, gr.nq, o + wave * M::TILE);
-      store_stat(t + gw * 32, buf);
-      load_stat(t + step + gw * 32);
+      for (int r = 0; r < 16; ++r) {
+        const uint32_t at = WIDE ? ((((b[r >> 2] >> (8 * (r & 3))) & 0xffu) << 7) | copy)
+                                 : __builtin_amdgcn_perm(b[r >> 2], copy, 0x0c0c0000u | ((4u + (r & 3)) << 8));
+        atomicAdd(reinterpret_cast<unsigned long long*>(reinterpret_cast<uint8_t*>(hist) + at),
+                  (unsigned long long)(long long)pack_round(x[r]));
+        if constexpr (CAP) x[r] *= slope[r];
+      }
+      M::cols(ot, p, dv);
+      M::cols(qt, x, dk);
     };
-    if constexpr (NB == 2) {
-      T* const sQ1 = reinterpret_cast<T*>(sBuf1);
-      T* const sO1 = sQ1 + kPackWaves * M::TILE;
-      if (jb.steps > 0) stage(sQ0, sO0, 0, t0);
-      for (int t = 0; t < jb.steps; t += 2) {
-        wait_vmcnt<0>();
-        lds_barrier();
-        if (t + 1 < jb.steps) stage(sQ1, sO1, 1, t0 + step);
-        blocks(sQ0, sO0, 0, t0);
-        t0 += step;
-        if (t + 1 >= jb.steps) break;
-        wait_vmcnt<0>();
-        lds_barrier();
-        if (t + 2 < jb.steps) stage(sQ0, sO0, 0, t0 + step);
-        blocks(sQ1, sO1, 1, t0);
-        t0 += step;
+    auto blocks = [&](const T* sQ, const T* sO, int buf, int t0) {
+      if (!active) return;
+      for (int ib = 0; ib < W; ++ib) {
+        const int i0 = t0 + ib * 32, slot = (grp << lw) + ib;
+        if (i0 >= gr.c1) break;
+        block(sQ + slot * M::TILE, sO + slot * M::TILE, sStat[buf][slot], i0);
+      }
+    };
+
+    int t0 = gr.c0;
+    T* const sQ0 = reinterpret_cast<T*>(sBuf0);
+    T* const sO0 = sQ0 + kPackWaves * M::TILE;
+    if (gr.steps > 0) {
+      load_stat(t0 + gw * 32);
+      fetch(t0, w);
+    }
+    if constexpr (M::BF16) {
+      const PackDma<M> cq(a.q.rs), co(a.d_o.rs);
+      auto stage = [&](T* q, T* o, int buf, int t) {
+        cq.load(qh, a.q.rs, t + gw * 32, gr.nq, q + wave * M::TILE);
+        co.load(oh, a.d_o.rs, t + gw * 32, gr.nq, o + wave * M::TILE);
+        store_stat(t + gw * 32, buf);
+        load_stat(t + step + gw * 32);
+      };
+      if constexpr (NB == 2) {
+        T* const sQ1 = reinterpret_cast<T*>(sBuf1);
+        T* const sO1 = sQ1 + kPackWaves * M::TILE;
+        if (gr.steps > 0) stage(sQ0, sO0, 0, t0);
+        for (int t = 0; t < gr.steps; t += 2) {
+          wait_vmcnt<0>();
+          lds_barrier();
+          if (t + 1 < gr.steps) stage(sQ1, sO1, 1, t0 + step);
+          blocks(sQ0, sO0, 0, t0);
+          t0 += step;
+          if (t + 1 >= gr.steps) break;
+          wait_vmcnt<0>();
+          lds_barrier();
+          if (t + 2 < gr.steps) stage(sQ0, sO0, 0, t0 + step);
+          blocks(sQ1, sO1, 1, t0);
+          t0 += step;
+        }
+      } else {
+        for (int t = 0; t < gr.steps; ++t, t0 += step) {
+          lds_barrier();
+          stage(sQ0, sO0, 0, t0);
+          wait_vmcnt<0>();
+          lds_barrier();
+          blocks(sQ0, sO0, 0, t0);
+        }
       }
     } else {
-      for (int t = 0; t < jb.steps; ++t, t0 += step) {
+      PackStage<M> tq, to;
+      auto load = [&](int t) {
+        tq.load(qh, a.q.rs, t + gw * 32, gr.nq);
+        to.load(oh, a.d_o.rs, t + gw * 32, gr.nq);
+      };
+      if (gr.steps > 0) load(t0);
+      for (int t = 0; t < gr.steps; ++t, t0 += step) {
         lds_barrier();
-        stage(sQ0, sO0, 0, t0);
-        wait_vmcnt<0>();
+        tq.store(sQ0 + wave * M::TILE);
+        to.store(sO0 + wave * M::TILE);
+        store_stat(t0 + gw * 32, 0);
         lds_barrier();
+        if (t + 1 < gr.steps) {
+          load(t0 + step);
+          load_stat(t0 + step + gw * 32);
+        }
         blocks(sQ0, sO0, 0, t0);
       }
     }
-  } else {
-    PackStage<M> tq, to;
-    auto load = [&](int t) {
-      tq.load(qh, a.q.rs, t + gw * 32, gr.nq);
-      to.load(oh, a.d_o.rs, t + gw * 32, gr.nq);
-    };
-    if (jb.steps > 0) load(t0);
-    for (int t = 0; t < jb.steps; ++t, t0 += step) {
-      lds_barrier();
-      tq.store(sQ0 + wave * M::TILE);
-      to.store(sO0 + wave * M::TILE);
-      store_stat(t0 + gw * 32, 0);
-      lds_barrier();
-      if (t + 1 < jb.steps) {
-        load(t0 + step);
-        load_stat(t0 + step + gw * 32);
-      }
-      blocks(sQ0, sO0, 0, t0);
-    }
-  }
-  {
     // a dS that is no number makes its key's dK so: the head's table gradient is
     // then NaN (the fixed-point sums cannot show it)
     bool ok = true;
 #pragma unroll
     for (int r = 0; r < 16; ++r) ok = ok && fabsf(dk[0][r]) < INFINITY;
-    const bool any_bad = __any(jok && !ok);
-    if (lane == 0) bad[wave] = any_bad;
+    any_bad = any_bad || __any(jok && !ok);
+    if (gr.combine) {
+      float* buf = reinterpret_cast<float*>(sBuf0);
+      auto none = [](int) {};
+      auto add = [](int, float& wa, float& wo) { wa = wo = 1.0f; };
+      pack_combine(buf, lw, grp, gw, dk, none, add);
+      pack_combine(buf, lw, grp, gw, dv, none, add);
+    }
+    if (jok && (!gr.combine || grp == 0)) {
+      T* dkp = rows_at<T>(a.dk, h, gr.k0 + j);
+      T* dvp = rows_at<T>(a.dv, h, gr.k0 + j);
+      M::features(dk, [&](int f, float4 x) { M::store4(dkp + f, make_float4(x.x * mk, x.y * mk, x.z * mk, x.w * mk)); });
+      M::features(dv, [&](int f, float4 x) { M::store4(dvp + f, make_float4(x.x * rp, x.y * rp, x.z * rp, x.w * rp)); });
+    }
+    lds_barrier();                                        // the next job stages over this one's tiles
   }
-  if (jb.combine) {
-    float* buf = reinterpret_cast<float*>(sBuf0);
-    auto none = [](int) {};
-    auto add = [](int, float& wa, float& wo) { wa = wo = 1.0f; };
-    pack_combine(buf, lw, grp, gw, dk, none, add);
-    pack_combine(buf, lw, grp, gw, dv, none, add);
-  }
-  const float rp = DROP ? a.rp : 1.0f;
-  if (jok && (!jb.combine || grp == 0)) {
-    const float mk = a.scale * rp * ldexpf(1.0f, -fexp) * (CAP ? M::kSlope : 1.0f);
-    T* dkp = rows_at<T>(a.dk, h, gr.k0 + j);
-    T* dvp = rows_at<T>(a.dv, h, gr.k0 + j);
-    M::features(dk, [&](int f, float4 x) { M::store4(dkp + f, make_float4(x.x * mk, x.y * mk, x.z * mk, x.w * mk)); });
-    M::features(dv, [&](int f, float4 x) { M::store4(dvp + f, make_float4(x.x * rp, x.y * rp, x.z * rp, x.w * rp)); });
-  }
+  if (lane == 0) bad[wave] = any_bad;
   __syncthreads();
   const double unscale = ldexp((double)rp, -fexp);
   const bool nan = bad[0] | bad[1] | bad[2] | bad[3];
@@ -376,17 +378,18 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_dkdv_kernel(PackArgs a) 
     long long t = 0;
 #pragma unroll
     for (int c = 0; c < CPY; ++c) t += (long long)hist[b * CPY + ((c + b) & (CPY - 1))];
-    a.dtab_part[((int64_t)h * a.njobs + pl.job) * a.n_buckets + b] = nan ? (double)NAN : (double)t * unscale;
+    a.dtab_part[((int64_t)h * a.slots + pl.job) * a.n_buckets + b] = nan ? (double)NAN : (double)t * unscale;
   }
 }
 
 template <class M, bool CAP, bool DROP>
-void launch_pack_dkdv_nb(const PackArgs& a, hipStream_t s) {
-  const dim3 grid(pack_grid(a.njobs, a.H)), block(kPackThreads);
-  if (a.n_buckets > 127)
-    hipLaunchKernelGGL((pack_dkdv_kernel<M, CAP, DROP, true>), grid, block, 0, s, a);
+void launch_pack_dkdv_nb(PackArgs a, hipStream_t s) {
+  const dim3 grid(pack_grid(a.slots, a.H)), block(kPackThreads);
+  a.hist = a.n_buckets < 32 ? 32 : (a.n_buckets < 64 ? 64 : (a.n_buckets < 128 ? 128 : 256));
+  if (a.hist == 256)
+    hipLaunchKernelGGL((pack_dkdv_kernel<M, CAP, DROP, true>), grid, block, 256 * 16 * 8, s, a);
   else
-    hipLaunchKernelGGL((pack_dkdv_kernel<M, CAP, DROP, false>), grid, block, 0, s, a);
+    hipLaunchKernelGGL((pack_dkdv_kernel<M, CAP, DROP, false>), grid, block, (unsigned)a.hist * 32 * 8, s, a);
 }
 
 template <class M>

@@ -34,14 +34,13 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_dq_kernel(PackArgs a) {
   __shared__ float sTab[256];
   __shared__ uint4 sKeys[DROP ? NB * kPackWaves * 4 : 1];
 
-  const PackPlace pl(a);
+  const PackPlace pl(a, a.njobs);
   if (pl.job >= a.njobs) return;
   const int h = pl.h;
-  const PackJob jb = scalar_record(a.jobs + pl.job);
   const int wave = wave_id(), lane = threadIdx.x & 63, col = lane & 31, g = lane >> 5;
-  const int lw = jb.log2w, W = 1 << lw;
+  const PackWave gr = scalar_record(a.jobs + (int64_t)pl.job * kPackWaves + wave);
+  const int lw = gr.log2w, W = 1 << lw;
   const int grp = wave >> lw, gw = wave & (W - 1);
-  const PackGroup gr = scalar_record(a.groups + jb.group + grp);
   constexpr bool START = M::BF16 && !CAP;
   ScoreRef ref{false, 0.0f};
   {
@@ -57,7 +56,7 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_dq_kernel(PackArgs a) {
   }
 
   const int off = gr.nk - gr.nq;
-  const int iw = gr.row0 + gw * 32;
+  const int iw = gr.row;
   const int i = iw + col;
   const bool active = iw < gr.nq;
   const bool iok = i < gr.nq;
@@ -170,7 +169,7 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_dq_kernel(PackArgs a) {
   int t0 = gr.c0;
   T* const sK0 = reinterpret_cast<T*>(sBuf0);
   T* const sV0 = sK0 + kPackWaves * M::TILE;
-  if (jb.steps > 0) spd.fetch(t0, w);
+  if (gr.steps > 0) spd.fetch(t0, w);
   if constexpr (M::BF16) {
     T* const sK1 = reinterpret_cast<T*>(sBuf1);
     T* const sV1 = sK1 + kPackWaves * M::TILE;
@@ -179,23 +178,23 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_dq_kernel(PackArgs a) {
       dk.load(kh, a.k.rs, t + gw * 32, gr.nk, k + wave * M::TILE);
       dv.load(vh, a.v.rs, t + gw * 32, gr.nk, v + wave * M::TILE);
     };
-    if (jb.steps > 0) {
+    if (gr.steps > 0) {
       copy(sK0, sV0, t0);
       put_keys(t0, 0);
     }
-    for (int t = 0; t < jb.steps; t += 2) {
+    for (int t = 0; t < gr.steps; t += 2) {
       wait_vmcnt<0>();
       lds_barrier();
-      if (t + 1 < jb.steps) {
+      if (t + 1 < gr.steps) {
         copy(sK1, sV1, t0 + step);
         put_keys(t0 + step, 1);
       }
       blocks(sK0, sV0, 0, t0);
       t0 += step;
-      if (t + 1 >= jb.steps) break;
+      if (t + 1 >= gr.steps) break;
       wait_vmcnt<0>();
       lds_barrier();
-      if (t + 2 < jb.steps) {
+      if (t + 2 < gr.steps) {
         copy(sK0, sV0, t0 + step);
         put_keys(t0 + step, 0);
       }
@@ -208,14 +207,14 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_dq_kernel(PackArgs a) {
       tk.load(kh, a.k.rs, t + gw * 32, gr.nk);
       tv.load(vh, a.v.rs, t + gw * 32, gr.nk);
     };
-    if (jb.steps > 0) load(t0);
-    for (int t = 0; t < jb.steps; ++t, t0 += step) {
+    if (gr.steps > 0) load(t0);
+    for (int t = 0; t < gr.steps; ++t, t0 += step) {
       lds_barrier();
       tk.store(sK0 + wave * M::TILE);
       tv.store(sV0 + wave * M::TILE);
       put_keys(t0, 0);
       lds_barrier();
-      if (t + 1 < jb.steps) load(t0 + step);
+      if (t + 1 < gr.steps) load(t0 + step);
       blocks(sK0, sV0, 0, t0);
     }
   }
@@ -226,7 +225,7 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_dq_kernel(PackArgs a) {
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) dmax = fmaxf(dmax, __shfl_xor(dmax, o));
   float2* dm = a.dmax + ((int64_t)h * a.njobs + pl.job) * kPackWaves + wave;
-  if (jb.combine) {
+  if (gr.combine) {
     float* stat = reinterpret_cast<float*>(sBuf0 + NA * 16 * 64 * 4 * 2) + lane;
     pack_combine(
         reinterpret_cast<float*>(sBuf0), lw, grp, gw, acc, [&](int slot) { stat[slot * 64] = dsum; },

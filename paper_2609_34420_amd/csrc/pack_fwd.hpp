@@ -30,14 +30,13 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_fwd_kernel(PackArgs a) {
   __shared__ float sTab[256];
   __shared__ uint4 sKeys[DROP ? NB * kPackWaves * 4 : 1];        // KeyDraws of the staged keys
 
-  const PackPlace pl(a);
+  const PackPlace pl(a, a.njobs);
   if (pl.job >= a.njobs) return;
   const int h = pl.h;
-  const PackJob jb = scalar_record(a.jobs + pl.job);
   const int wave = wave_id(), lane = threadIdx.x & 63, col = lane & 31, g = lane >> 5;
-  const int lw = jb.log2w, W = 1 << lw;
+  const PackWave gr = scalar_record(a.jobs + (int64_t)pl.job * kPackWaves + wave);
+  const int lw = gr.log2w, W = 1 << lw;
   const int grp = wave >> lw, gw = wave & (W - 1);
-  const PackGroup gr = scalar_record(a.groups + jb.group + grp);
   constexpr bool START = M::BF16 && !CAP;              // the score accumulator starts from the bias
   ScoreRef fix{false, 0.0f};
   {
@@ -53,7 +52,7 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_fwd_kernel(PackArgs a) {
   }
 
   const int off = gr.nk - gr.nq;
-  const int iw = gr.row0 + gw * 32;                    // the wave's first query
+  const int iw = gr.row;                    // the wave's first query
   const int i = iw + col;
   const bool active = iw < gr.nq;
   const bool iok = i < gr.nq;
@@ -164,7 +163,7 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_fwd_kernel(PackArgs a) {
   int t0 = gr.c0;                                      // the tile's first key
   T* const sK0 = reinterpret_cast<T*>(sBuf0);
   T* const sV0 = sK0 + kPackWaves * M::TILE;
-  if (jb.steps > 0) spd.fetch(t0, w);
+  if (gr.steps > 0) spd.fetch(t0, w);
   if constexpr (M::BF16) {
     const PackDma<M> dk(a.k.rs), dv(a.v.rs);
     auto copy = [&](T* k, T* v, int t) {
@@ -172,7 +171,7 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_fwd_kernel(PackArgs a) {
       dv.load(vh, a.v.rs, t + gw * 32, gr.nk, v + wave * M::TILE);
     };
     if constexpr (NB == 1) {
-      for (int t = 0; t < jb.steps; ++t, t0 += step) {
+      for (int t = 0; t < gr.steps; ++t, t0 += step) {
         lds_barrier();                                 // the last tile's reads are done
         copy(sK0, sV0, t0);
         put_keys(t0, 0);
@@ -184,23 +183,23 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_fwd_kernel(PackArgs a) {
     }
     T* const sK1 = reinterpret_cast<T*>(sBuf1);
     T* const sV1 = sK1 + (NB == 2 ? kPackWaves * M::TILE : 0);
-    if (NB == 2 && jb.steps > 0) {
+    if (NB == 2 && gr.steps > 0) {
       copy(sK0, sV0, t0);
       put_keys(t0, 0);
     }
-    for (int t = 0; NB == 2 && t < jb.steps; t += 2) {
+    for (int t = 0; NB == 2 && t < gr.steps; t += 2) {
       wait_vmcnt<0>();
       lds_barrier();                                   // the tile has landed, the last one's reads are done
-      if (t + 1 < jb.steps) {
+      if (t + 1 < gr.steps) {
         copy(sK1, sV1, t0 + step);
         put_keys(t0 + step, 1);
       }
       blocks(sK0, sV0, 0, t0);
       t0 += step;
-      if (t + 1 >= jb.steps) break;
+      if (t + 1 >= gr.steps) break;
       wait_vmcnt<0>();
       lds_barrier();
-      if (t + 2 < jb.steps) {
+      if (t + 2 < gr.steps) {
         copy(sK0, sV0, t0 + step);
         put_keys(t0 + step, 0);
       }
@@ -213,20 +212,20 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_fwd_kernel(PackArgs a) {
       tk.load(kh, a.k.rs, t + gw * 32, gr.nk);
       tv.load(vh, a.v.rs, t + gw * 32, gr.nk);
     };
-    if (jb.steps > 0) load(t0);
-    for (int t = 0; t < jb.steps; ++t, t0 += step) {
+    if (gr.steps > 0) load(t0);
+    for (int t = 0; t < gr.steps; ++t, t0 += step) {
       lds_barrier();                                   // the last tile's reads are done
       tk.store(sK0 + wave * M::TILE);
       tv.store(sV0 + wave * M::TILE);
       put_keys(t0, 0);
       lds_barrier();
-      if (t + 1 < jb.steps) load(t0 + step);
+      if (t + 1 < gr.steps) load(t0 + step);
       blocks(sK0, sV0, 0, t0);
     }
   }
   l += __shfl_xor(l, 32);
   if (fix.fixed) m = l == 0.0f ? -INFINITY : fix.ref;
-  if (jb.combine) {
+  if (gr.combine) {
     float2* stat = reinterpret_cast<float2*>(sBuf0 + NA * 16 * 64 * 4 * 2) + lane;
     pack_combine(
         reinterpret_cast<float*>(sBuf0), lw, grp, gw, acc, [&](int slot) { stat[slot * 64] = make_float2(m, l); },

@@ -31,9 +31,18 @@ struct Graph {
   int64_t spd;
 };
 
+// A group of a job before its waves are written out.
+struct Group {
+  int32_t graph, row0, c0, c1, part;
+};
+struct Job {
+  int32_t group;       // first of its 4 / W groups
+  int32_t log2w, combine, steps;
+};
+
 struct Plan {
-  std::vector<PackGroup> groups;
-  std::vector<PackJob> jobs;
+  std::vector<Group> groups;
+  std::vector<Job> jobs;
   std::vector<PackMerge> merges;
   int32_t parts = 0;
 };
@@ -54,7 +63,7 @@ void columns(const Graph& g, Stage st, int32_t row0, int32_t rows, int32_t& c0, 
 }
 
 struct Item {
-  PackGroup g;
+  Group g;
   int32_t cost;       // blocks per wave
 };
 
@@ -62,16 +71,16 @@ struct Item {
 Plan build(const std::vector<Graph>& graphs, int32_t H, Stage st, int s) {
   Plan p;
   std::vector<std::vector<Item>> whole(3);         // by log2w: groups that share a workgroup with others
-  std::vector<std::pair<int32_t, PackJob>> jobs;   // cost, job
+  std::vector<std::pair<int32_t, Job>> jobs;       // cost, job
   std::vector<std::pair<Item, int>> split;         // combined: item, log2w
-  for (const Graph& g : graphs) {
+  for (size_t gi = 0; gi < graphs.size(); ++gi) {
+    const Graph& g = graphs[gi];
     const int32_t rows = st == kDkdv ? g.nk : g.nq;
     int lw = s == 1 ? 2 : (s == 2 ? 1 : 0);
     while (lw > 0 && rows <= (32 << (lw - 1))) --lw;
     const int32_t step = 32 << lw;
     for (int64_t r = 0; r < rows; r += step) {
-      Item it{};
-      it.g = PackGroup{g.q0, g.nq, g.k0, g.nk, (int32_t)r, 0, 0, g.prefix, g.spd, g.ld, -1};
+      Item it{{(int32_t)gi, (int32_t)r, 0, 0, -1}, 0};
       columns(g, st, (int32_t)r, step, it.g.c0, it.g.c1);
       it.cost = (it.g.c1 - it.g.c0 + 31) / 32;
       if (s == 1)
@@ -85,9 +94,9 @@ Plan build(const std::vector<Graph>& graphs, int32_t H, Stage st, int s) {
     std::stable_sort(w.begin(), w.end(), [](const Item& a, const Item& b) { return a.cost > b.cost; });
     const int n = kPackWaves >> lw;
     for (size_t i = 0; i < w.size(); i += n) {
-      PackJob j{(int32_t)p.groups.size(), lw, 0, (w[i].cost + (1 << lw) - 1) >> lw};
+      const Job j{(int32_t)p.groups.size(), lw, 0, (w[i].cost + (1 << lw) - 1) >> lw};
       for (int k = 0; k < n; ++k)
-        p.groups.push_back(i + k < w.size() ? w[i + k].g : PackGroup{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, -1});
+        p.groups.push_back(i + k < w.size() ? w[i + k].g : Group{-1, 0, 0, 0, -1});
       jobs.push_back({w[i].cost, j});
     }
   }
@@ -116,14 +125,15 @@ Plan build(const std::vector<Graph>& graphs, int32_t H, Stage st, int s) {
     per_part = (per_part + unit - 1) / unit * unit;
     parts = per_part > 0 ? std::max(1, (cols + per_part - 1) / per_part) : 1;
     if (parts > 1) {
-      p.merges.push_back({it.g.q0 + it.g.row0, std::min(32 << lw, it.g.nq - it.g.row0), p.parts, parts});
+      const Graph& g = graphs[it.g.graph];
+      p.merges.push_back({g.q0 + it.g.row0, std::min(32 << lw, g.nq - it.g.row0), p.parts, parts});
     }
     for (int32_t k = 0; k < parts; ++k) {
       const int32_t a = it.g.c0 + k * per_part, b = parts == 1 ? it.g.c1 : std::min(it.g.c1, a + per_part);
-      int32_t per = ((b - a + n - 1) / n + (32 << lw) - 1) / (32 << lw) * (32 << lw);
-      PackJob j{(int32_t)p.groups.size(), lw, n > 1 ? 1 : 0, per / (32 << lw)};
+      const int32_t per = ((b - a + n - 1) / n + (32 << lw) - 1) / (32 << lw) * (32 << lw);
+      const Job j{(int32_t)p.groups.size(), lw, n > 1 ? 1 : 0, per / (32 << lw)};
       for (int i = 0; i < n; ++i) {
-        PackGroup g = it.g;
+        Group g = it.g;
         g.c0 = (int32_t)std::min<int64_t>(a + (int64_t)i * per, b > a ? (b + 31) / 32 * 32 : a);
         g.c1 = (int32_t)std::max<int64_t>(g.c0, std::min<int64_t>(a + (int64_t)(i + 1) * per, b));
         g.part = parts > 1 ? p.parts : -1;
@@ -134,17 +144,28 @@ Plan build(const std::vector<Graph>& graphs, int32_t H, Stage st, int s) {
     }
   }
   std::stable_sort(jobs.begin(), jobs.end(),
-                   [](const std::pair<int32_t, PackJob>& a, const std::pair<int32_t, PackJob>& b) {
-                     return a.first > b.first;
-                   });
+                   [](const std::pair<int32_t, Job>& a, const std::pair<int32_t, Job>& b) { return a.first > b.first; });
   for (auto& j : jobs) p.jobs.push_back(j.second);
   return p;
+}
+
+std::vector<PackWave> waves(const std::vector<Graph>& graphs, const Plan& p) {
+  std::vector<PackWave> out;
+  out.reserve(p.jobs.size() * kPackWaves);
+  for (const Job& j : p.jobs)
+    for (int w = 0; w < kPackWaves; ++w) {
+      const Group& g = p.groups[j.group + (w >> j.log2w)];
+      const Graph x = g.graph >= 0 ? graphs[g.graph] : Graph{};
+      out.push_back({x.q0, x.nq, x.k0, x.nk, g.row0 + (w & ((1 << j.log2w) - 1)) * 32, g.c0, g.c1, x.prefix, x.spd,
+                     x.ld, g.part, j.log2w, j.combine, j.steps, 0});
+    }
+  return out;
 }
 
 // The longest workgroup, or the chip's share of all of them.
 double span(const Plan& p, int32_t H) {
   double sum = 0.0, top = 0.0;
-  for (const PackJob& j : p.jobs) {
+  for (const Job& j : p.jobs) {
     const double c = (double)j.steps * (1 << j.log2w) + kSetup;
     sum += c;
     top = std::max(top, c);
@@ -164,6 +185,19 @@ Plan best_plan(const std::vector<Graph>& graphs, int32_t H, Stage st) {
     }
   }
   return best;
+}
+
+// Workgroups per head of the key-stationary kernel, which take one job after the
+// other: the table, the histogram and its sums cost about as much as 16 blocks,
+// so short jobs share a workgroup as long as the chip stays full. Long ones get one
+// each, dealt out longest first as workgroups end.
+int32_t slots(const Plan& p, int32_t H) {
+  const int64_t n = (int64_t)p.jobs.size();
+  int64_t sum = 0;
+  for (const Job& j : p.jobs) sum += (int64_t)j.steps << j.log2w;
+  const int64_t by_work = (sum + 15) / 16;
+  const int64_t full = (kSlots + H - 1) / H;
+  return (int32_t)std::min(n, std::max(by_work, full));
 }
 
 template <typename T>
@@ -206,22 +240,25 @@ gt_status_t make(int32_t G, int32_t H, const int32_t* n_q, const int32_t* n_k, c
   }
   info.n_graphs = G;
   info.H = H;
-  Plan plans[3];
+  std::vector<PackWave> lists[3];
+  std::vector<PackMerge> merges;
   const Stage stages[3] = {kForward, kDq, kDkdv};
   for (int i = 0; i < 3; ++i) {
-    plans[i] = best_plan(graphs, H, stages[i]);
-    if (((int64_t)plans[i].jobs.size() + 8) * H > std::numeric_limits<int32_t>::max()) return GT_ERR_UNSUPPORTED;
+    const Plan p = best_plan(graphs, H, stages[i]);
+    if (((int64_t)p.jobs.size() + 8) * H > std::numeric_limits<int32_t>::max()) return GT_ERR_UNSUPPORTED;
+    lists[i] = waves(graphs, p);
+    info.jobs[i] = (int32_t)p.jobs.size();
+    if (i == kForward) {
+      merges = p.merges;
+      info.merges = (int32_t)merges.size();
+      info.parts = p.parts;
+    }
+    if (i == kDkdv) info.slots = slots(p, H);
   }
   auto lay_out = [&](uint8_t* buf) {
     size_t at = 0;
-    for (int i = 0; i < 3; ++i) {
-      info.jobs[i] = (int32_t)plans[i].jobs.size();
-      info.job_off[i] = place(at, plans[i].jobs, buf);
-      info.group_off[i] = place(at, plans[i].groups, buf);
-    }
-    info.merges = (int32_t)plans[kForward].merges.size();
-    info.parts = plans[kForward].parts;
-    info.merge_off = place(at, plans[kForward].merges, buf);
+    for (int i = 0; i < 3; ++i) info.job_off[i] = place(at, lists[i], buf);
+    info.merge_off = place(at, merges, buf);
     info.plan_bytes = (int64_t)at;
   };
   lay_out(nullptr);

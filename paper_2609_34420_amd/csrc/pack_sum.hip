@@ -49,14 +49,14 @@ __global__ __launch_bounds__(256) void pack_merge_kernel(PackArgs a, int d) {
   }
 }
 
-// dtable[h, b]: the jobs' sums in a fixed order, 16 threads per bucket.
+// dtable[h, b]: the workgroups' sums in a fixed order, 16 threads per bucket.
 __global__ __launch_bounds__(256) void pack_dtable_kernel(PackArgs a) {
   __shared__ double red[256];
   const int h = blockIdx.y, b = blockIdx.x * 16 + threadIdx.x % 16;
   double s = 0.0;
   if (b < a.n_buckets)
-    for (int j = threadIdx.x / 16; j < a.njobs; j += 16)
-      s += a.dtab_part[((int64_t)h * a.njobs + j) * a.n_buckets + b];
+    for (int j = threadIdx.x / 16; j < a.slots; j += 16)
+      s += a.dtab_part[((int64_t)h * a.slots + j) * a.n_buckets + b];
   red[threadIdx.x] = s;
   __syncthreads();
   if (threadIdx.x < 16 && b < a.n_buckets) {

@@ -48,7 +48,7 @@ class _Rows(ctypes.Structure):
 class _Info(ctypes.Structure):
     _fields_ = [("total_q", _I64), ("total_k", _I64), ("spd_bytes", _I64), ("plan_bytes", _I64),
                 ("n_graphs", _I32), ("H", _I32), ("jobs", _I32 * 3), ("merges", _I32), ("parts", _I32),
-                ("reserved", _I32), ("job_off", _I64 * 3), ("group_off", _I64 * 3), ("merge_off", _I64)]
+                ("slots", _I32), ("job_off", _I64 * 3), ("merge_off", _I64)]
 
 
 class _Dropout(ctypes.Structure):
@@ -113,9 +113,9 @@ def gt_attn_pack(n_q, H: int, n_k=None, prefix=None, spd_off=None, spd_ld=None, 
                                        None if buf is None else buf.ctypes.data,
                                        0 if buf is None else buf.nbytes, ctypes.byref(info))
 
-    # (about 64 bytes per 32 rows and list in most plans; a second call where it is more)
+    # (64 bytes per 32 rows and list in most plans; a second call where it is more)
     blocks = int((nq.astype(np.int64) + 31).sum() + (nk.astype(np.int64) + 31).sum()) // 32
-    buf = np.empty(4096 + 256 * (blocks + nq.size), dtype=np.uint8)
+    buf = np.empty(8192 + 192 * blocks + 512 * min(nq.size, 64), dtype=np.uint8)
     st = call(buf)
     if st == 3 and info.plan_bytes > buf.nbytes:
         buf = np.empty(info.plan_bytes, dtype=np.uint8)

@@ -8,9 +8,8 @@ import torch
 
 import paper_2609_34420_amd as gt
 
-GROUP = np.dtype([(n, "<i4") for n in ("q0", "nq", "k0", "nk", "row0", "c0", "c1", "prefix")]
-                 + [("spd", "<i8"), ("ld", "<i4"), ("part", "<i4")])
-JOB = np.dtype([(n, "<i4") for n in ("group", "log2w", "combine", "steps")])
+WAVE = np.dtype([(n, "<i4") for n in ("q0", "nq", "k0", "nk", "row", "c0", "c1", "prefix")]
+                + [("spd", "<i8")] + [(n, "<i4") for n in ("ld", "part", "log2w", "combine", "steps", "pad")])
 MERGE = np.dtype([(n, "<i4") for n in ("row", "rows", "part", "parts")])
 FULL = np.iinfo(np.int32).max
 
@@ -19,9 +18,7 @@ def lists(pack):
     i, buf = pack._info, pack._plan.numpy()
     out = []
     for s in range(3):
-        jobs = buf[i.job_off[s]:].view(np.uint8)[:i.jobs[s] * JOB.itemsize].view(JOB)
-        n = sum(4 >> j["log2w"] for j in jobs)
-        out.append((jobs, buf[i.group_off[s]:][:n * GROUP.itemsize].view(GROUP)))
+        out.append(buf[i.job_off[s]:][:4 * i.jobs[s] * WAVE.itemsize].view(WAVE).reshape(-1, 4))
     return out, buf[i.merge_off:][:i.merges * MERGE.itemsize].view(MERGE)
 
 
@@ -40,17 +37,24 @@ def check(n_q, n_k, prefix, H):
             starts[(a, x, b, y)] = g
         a, b, s = a + x, b + y, s + x * y
     assert (pack.total_q, pack.total_k) == (a, b)
-    for st, (jobs, groups) in enumerate(stages):
+    assert 0 < pack._info.slots <= len(stages[2]) or len(stages[2]) == 0
+    for st, jobs in enumerate(stages):
         seen = [np.zeros((x, y), np.int32) for x, y in zip(n_q, n_k)]
         rows_done = [np.zeros(y if st == 2 else x, np.int32) for x, y in zip(n_q, n_k)]
         parts = {}
-        for job in jobs:
+        for waves in jobs:
+            job = waves[0]
             w = 1 << job["log2w"]
             assert w in (1, 2, 4)
-            mine = groups[job["group"]:job["group"] + 4 // w]
-            assert len(mine) == 4 // w
+            same = [n for n in WAVE.names if n != "row"]
+            for k in range(0, 4, w):                       # a group's waves: 32 rows after 32 rows
+                for e in range(w):
+                    assert all(waves[k + e][n] == waves[k][n] for n in same)
+                    assert waves[k + e]["row"] == waves[k]["row"] + 32 * e
+            assert all(x[n] == job[n] for x in waves for n in ("log2w", "combine", "steps"))
+            mine = waves[::w]
             if job["combine"]:
-                assert len({(x["q0"], x["nq"], x["k0"], x["nk"], x["row0"], x["part"]) for x in mine}) == 1
+                assert len({(x["q0"], x["nq"], x["k0"], x["nk"], x["row"], x["part"]) for x in mine}) == 1
             for k, x in enumerate(mine):
                 n_rows, n_cols = (x["nk"], x["nq"]) if st == 2 else (x["nq"], x["nk"])
                 if n_rows == 0 and n_cols == 0:
@@ -59,10 +63,10 @@ def check(n_q, n_k, prefix, H):
                 g = starts[(x["q0"], x["nq"], x["k0"], x["nk"])]
                 assert x["prefix"] == (FULL if prefix is None else prefix[g]) and x["ld"] == n_k[g]
                 assert x["spd"] == sum(p * q for p, q in zip(n_q[:g], n_k[:g]))
-                assert x["row0"] % 32 == 0 and x["c0"] % 32 == 0 and 0 <= x["c0"] <= x["c1"] or x["c0"] >= x["c1"]
+                assert x["row"] % 32 == 0 and x["c0"] % 32 == 0 and 0 <= x["c0"] <= x["c1"] or x["c0"] >= x["c1"]
                 assert x["c1"] <= n_cols or x["c0"] >= x["c1"]
                 assert job["steps"] * 32 * w >= x["c1"] - x["c0"]
-                r = slice(x["row0"], min(n_rows, x["row0"] + 32 * w))
+                r = slice(x["row"], min(n_rows, x["row"] + 32 * w))
                 c = slice(x["c0"], max(x["c0"], x["c1"]))
                 if st == 2:
                     seen[g][c, r] += 1
