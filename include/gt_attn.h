@@ -416,7 +416,7 @@ size_t gt_attn_pack_bwd_workspace_size(const gt_attn_pack_t* pack, int32_t n_buc
  *   q [H, >= total_q, d], k, v [H, >= total_k, d] dtype; o as q (written)
  *   spd    >= pack->spd_bytes bytes    table [H, n_buckets] fp32
  *   lse    [H, ld_lse] fp32 (written), ld_lse >= total_q
- *   cap    0 (no cap), or positive and finite
+ *   cap    0 (no cap), or in 2^-10 .. 2^10 (scores are off by up to about 2^-21 cap)
  *   dropout NULL: none
  * Otherwise as gt_attn_fwd. Deterministic. */
 gt_status_t gt_attn_pack_fwd(const gt_attn_pack_t* pack, const void* plan, const gt_attn_rows_t* q,

@@ -382,26 +382,40 @@ struct F32Pack {
   __device__ __forceinline__ static float entry(float bias, const PackArgs&, bool) {
     return bias <= kNoScore ? -INFINITY : bias;
   }
-  // x = S. (The entries are added after the product: as the accumulator's
-  // start they would raise the rounding of every step.) tanh by its series up to
-  // 0.3 (next term 5e-8 of it), else 1 - 2 / (e^(2 y) + 1), off by about 2^-23 against a
-  // value of at least 0.29.
+  // x = S. (The entries are added after the product: as the accumulator's start they
+  // would raise the rounding of every step.) tanh(y) / y is a polynomial in y^2 up to
+  // |y| = 0.75, off by 3e-8 of it (fitted to the least largest relative error); beyond,
+  // 1 - 2 / (e^(2 y) + 1) is off by about 2^-23 against a value of at least 0.63. Blocks
+  // whose scores all stay below take the polynomial alone.
   template <bool CAP, bool SLOPE>
   __device__ __forceinline__ static void scores(const f32x16& s, float (&x)[16], float (&slope)[16],
                                                 const ScoreConst& c) {
+    if constexpr (!CAP) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] += s[r];
+      return;
+    }
+    float top = 0.0f, t[16];
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      if constexpr (!CAP) {
-        x[r] += s[r];
-      } else {
-        const float y = s[r], y2 = y * y;
-        const float small = y * fmaf(y2, fmaf(y2, fmaf(y2, fmaf(y2, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f),
-                                              -1.0f / 3.0f), 1.0f);
-        const float big = fmaf(-2.0f, 1.0f / (exp2_fast(fabsf(y) * (2.0f * kLog2e)) + 1.0f), 1.0f);
-        const float t = fabsf(y) < 0.3f ? small : copysignf(big, y);
-        if constexpr (SLOPE) slope[r] = fmaf(-t, t, 1.0f);
-        x[r] = fmaf(c.cap, t, x[r]);
+      const float y = s[r], z = y * y;
+      const float k = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -0.00471626f, 0.01958291f), -0.05334443f), 0.13325406f),
+                                   -0.33332959f), 0.99999997f);
+      t[r] = y * k;
+      top = fmaxf(top, z);
+    }
+    if (__any(!(top <= 0.5625f))) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float y = fabsf(s[r]);
+        const float big = fmaf(-2.0f, __builtin_amdgcn_rcpf(exp2_fast(y * (2.0f * kLog2e)) + 1.0f), 1.0f);
+        t[r] = y <= 0.75f ? t[r] : copysignf(big, s[r]);
       }
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      if constexpr (SLOPE) slope[r] = fmaf(-t[r], t[r], 1.0f);
+      x[r] = fmaf(c.cap, t[r], x[r]);
     }
   }
   static constexpr float kSlope = 1.0f;

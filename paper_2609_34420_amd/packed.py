@@ -45,6 +45,12 @@ class _Rows(ctypes.Structure):
     _fields_ = [("p", _P), ("head_stride", _I64), ("row_stride", _I64)]
 
 
+# A call's rows arguments are one array of their fields, passed by address (a
+# structure object for each takes half a microsecond of a small call's ten).
+_ROWS_BYTES = ctypes.sizeof(_Rows)
+_Rows4, _Rows8 = _I64 * 12, _I64 * 24
+
+
 class _Info(ctypes.Structure):
     _fields_ = [("total_q", _I64), ("total_k", _I64), ("spd_bytes", _I64), ("plan_bytes", _I64),
                 ("n_graphs", _I32), ("H", _I32), ("jobs", _I32 * 3), ("merges", _I32), ("parts", _I32),
@@ -56,8 +62,7 @@ class _Dropout(ctypes.Structure):
 
 
 def _register(L: ctypes.CDLL) -> None:
-    R, Z = ctypes.POINTER(_Rows), ctypes.c_size_t
-    info, drop = ctypes.POINTER(_Info), ctypes.POINTER(_Dropout)
+    R, Z, info, drop = _P, ctypes.c_size_t, _P, _P
     L.gt_attn_pack_plan.restype = _I32
     L.gt_attn_pack_plan.argtypes = [_I32, _I32, _P, _P, _P, _P, _P, _P, Z, info]
     L.gt_attn_pack_fwd_workspace_size.restype = Z
@@ -77,7 +82,11 @@ class GTPack:
 
     def __init__(self, info: _Info, plan: torch.Tensor):
         self._info = info
+        self._at = ctypes.addressof(info)
         self._plan = plan
+        self._plan_at = plan.data_ptr()
+        self._device_index = plan.get_device()
+        self._ws = {}                                   # workspace sizes by what they depend on beside the plan
         self.total_q, self.total_k = info.total_q, info.total_k
         self.spd_bytes, self.H, self.n_graphs = info.spd_bytes, info.H, info.n_graphs
         self.device = plan.device
@@ -125,33 +134,46 @@ def gt_attn_pack(n_q, H: int, n_k=None, prefix=None, spd_off=None, spd_ld=None, 
 
 
 def gt_attn_pack_fwd_workspace_size(pack: GTPack, d: int) -> int:
-    return int(lib().gt_attn_pack_fwd_workspace_size(ctypes.byref(pack._info), d))
+    n = pack._ws.get(("fwd", d))
+    if n is None:
+        n = pack._ws["fwd", d] = int(lib().gt_attn_pack_fwd_workspace_size(pack._at, d))
+    return n
 
 
 def gt_attn_pack_bwd_workspace_size(pack: GTPack, n_buckets: int) -> int:
-    return int(lib().gt_attn_pack_bwd_workspace_size(ctypes.byref(pack._info), n_buckets))
+    n = pack._ws.get(("bwd", n_buckets))
+    if n is None:
+        n = pack._ws["bwd", n_buckets] = int(lib().gt_attn_pack_bwd_workspace_size(pack._at, n_buckets))
+    return n
 
 
-def _rows(t, name: str, H: int, rows: int, d: int, dtype, written: bool = False) -> _Rows:
-    """A [H, >= rows, d] tensor as the C ABI's rows."""
+def _rows(t, name: str, H: int, rows: int, d: int, dtype, dev: int, written: bool = False) -> tuple:
+    """A [H, >= rows, d] tensor as the fields of the C ABI's rows."""
     if not isinstance(t, torch.Tensor) or t.dim() != 3:
         raise ValueError(f"{name} must be a 3-D tensor")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    n = t.shape[1]
-    if t.shape[0] != H or t.shape[2] != d or n < rows:
-        raise ValueError(f"{name} must have shape ({H}, >= {rows}, {d}), got {tuple(t.shape)}")
-    hs, rs, one = t.stride()
-    unit = 8 if dtype == torch.bfloat16 else 4
-    if one != 1 or (rows > 1 and (rs % unit or not d <= rs <= 1 << 23)) or (H > 1 and (hs % unit or hs < 0)):
-        raise ValueError(f"{name} must have unit feature stride, and row and head strides that are multiples of 16 "
-                         f"bytes, the row stride in {d}..{1 << 23}; got {t.stride()}")
-    if t.data_ptr() % 16:
+    h, n, w = t.shape
+    if h != H or w != d or n < rows:
+        raise ValueError(f"{name} must have shape ({H}, >= {rows}, {d}), got ({h}, {n}, {w})")
+    p = t.data_ptr()
+    if p % 16:
         raise ValueError(f"{name} must be 16-byte aligned")
-    if written and H > 1 and rows > 0 and not (hs >= (rows - 1) * rs + d or rs >= (H - 1) * hs + d and hs >= d):
-        raise ValueError(f"{name} is written: its rows must not overlap")
-    # (a stride that no element is reached by may be anything in torch)
-    return _Rows(t.data_ptr(), hs if H > 1 else 0, rs if rows > 1 else max(d, unit))
+    if t.is_contiguous():
+        hs, rs = n * d, d
+    else:
+        hs, rs, one = t.stride()
+        unit = 8 if dtype == torch.bfloat16 else 4
+        if one != 1 or (rows > 1 and (rs % unit or not d <= rs <= 1 << 23)) or (H > 1 and (hs % unit or hs < 0)):
+            raise ValueError(f"{name} must have unit feature stride, and row and head strides that are multiples of "
+                             f"16 bytes, the row stride in {d}..{1 << 23}; got {t.stride()}")
+        if written and H > 1 and rows > 0 and not (hs >= (rows - 1) * rs + d or (rs >= (H - 1) * hs + d and hs >= d)):
+            raise ValueError(f"{name} is written: its rows must not overlap")
+        # (a stride that no element is reached by may be anything in torch)
+        hs, rs = hs if H > 1 else 0, rs if rows > 1 else d
+    if dev >= 0 and t.get_device() != dev:
+        raise ValueError("tensors must be device tensors on one device")
+    return p, hs, rs
 
 
 def _dropout(dropout, dev: int):
@@ -176,22 +198,28 @@ def _common(q, k, v, spd, table, pack, scale, cap):
     else:
         dt = _qdims(q, "q", 3)
     H, _, d = q.shape
-    _need(H == pack.H, f"the plan is for {pack.H} heads, q has {H}")
-    rows = [_rows(q, "q", H, pack.total_q, d, dt), _rows(k, "k", H, pack.total_k, d, dt),
-            _rows(v, "v", H, pack.total_k, d, dt)]
-    _need(k.shape == v.shape, "k and v must have one shape")
+    if H != pack.H:
+        raise ValueError(f"the plan is for {pack.H} heads, q has {H}")
+    rows = (*_rows(q, "q", H, pack.total_q, d, dt, -1), *_rows(k, "k", H, pack.total_k, d, dt, -1),
+            *_rows(v, "v", H, pack.total_k, d, dt, -1))
+    if k.shape != v.shape:
+        raise ValueError("k and v must have one shape")
     if not (isinstance(spd, torch.Tensor) and spd.dtype == torch.uint8 and spd.is_contiguous()
             and spd.numel() >= pack.spd_bytes):
         raise ValueError(f"spd must be a contiguous uint8 tensor of at least {pack.spd_bytes} bytes")
     _table(table, H)
-    _need(table.is_contiguous(), "table must be contiguous")
-    _need(q.is_cuda, "tensors must be device tensors")
+    if not table.is_contiguous():
+        raise ValueError("table must be contiguous")
     dev = q.get_device()
-    _need(pack._plan.get_device() == dev, "the plan must be on q's device")
+    if dev < 0:
+        raise ValueError("tensors must be device tensors")
+    if pack._device_index != dev:
+        raise ValueError("the plan must be on q's device")
     _same_device(dev, k, v, spd, table)
     scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
     cap = 0.0 if cap is None else float(cap)
-    _need(0.0 <= cap < math.inf, f"cap must be positive and finite, or None, got {cap}")
+    if cap != 0.0 and not 2.0 ** -10 <= cap <= 1024.0:
+        raise ValueError(f"cap must lie in 2^-10..2^10, or be None, got {cap}")
     return dt, H, d, dev, rows, scale, cap
 
 
@@ -202,8 +230,9 @@ def _same_device(dev: int, *ts):
 
 
 def _lse(lse, H: int, T: int):
-    _need(isinstance(lse, torch.Tensor) and lse.dtype == torch.float32 and lse.shape == (H, T) and lse.is_contiguous(),
-          f"lse must be a contiguous float32 tensor of shape ({H}, {T})")
+    if not (isinstance(lse, torch.Tensor) and lse.dtype == torch.float32 and lse.shape == (H, T)
+            and lse.is_contiguous()):
+        raise ValueError(f"lse must be a contiguous float32 tensor of shape ({H}, {T})")
 
 
 def _on_stream(dev: int, stream, *held):
@@ -235,9 +264,9 @@ def gt_attn_pack_fwd(q, k, v, spd, table, pack: GTPack, scale: float | None = No
     gt_attn_pack_fwd). cap: bound of the scores before the bias, None for none;
     dropout: GTDropout or None. Rows behind the batch's total stay as they are
     (uninitialised where the call allocates)."""
-    dt, H, d, dev, (rq, rk, rv), scale, cap = _common(q, k, v, spd, table, pack, scale, cap)
+    dt, H, d, dev, rows, scale, cap = _common(q, k, v, spd, table, pack, scale, cap)
     T = q.shape[1]
-    drop = _dropout(dropout, dev)
+    drop = None if dropout is None else _dropout(dropout, dev)
     made = []
     if out is None:
         out = torch.empty((H, T, d), device=q.device, dtype=dt)
@@ -245,9 +274,11 @@ def gt_attn_pack_fwd(q, k, v, spd, table, pack: GTPack, scale: float | None = No
     if lse is None:
         lse = torch.empty((H, T), device=q.device, dtype=torch.float32)
         made.append(lse)
-    ro = _rows(out, "out", H, pack.total_q, d, dt, written=True)
-    _lse(lse, H, T)
-    _same_device(dev, out, lse)
+    else:
+        _lse(lse, H, T)
+        _same_device(dev, lse)
+    r = _Rows4(*rows, *_rows(out, "out", H, pack.total_q, d, dt, dev, written=True))
+    at = ctypes.addressof(r)
     need = gt_attn_pack_fwd_workspace_size(pack, d)
     if workspace is not None:
         _workspace(workspace, need, q)
@@ -255,10 +286,9 @@ def gt_attn_pack_fwd(q, k, v, spd, table, pack: GTPack, scale: float | None = No
         workspace = torch.empty(need, device=q.device, dtype=torch.uint8)
         made.append(workspace)
     s = _on_stream(dev, stream, pack._plan, *made)
-    b = ctypes.byref
-    st = _launch(dev, lib().gt_attn_pack_fwd, b(pack._info), _ptr(pack._plan), b(rq), b(rk), b(rv), _ptr(spd),
-                 _ptr(table), table.shape[1], b(ro), _ptr(lse), T, _ptr(workspace),
-                 0 if workspace is None else workspace.numel(), d, _dt(q), scale, cap, drop, s)
+    st = _launch(dev, lib().gt_attn_pack_fwd, pack._at, pack._plan_at, at, at + _ROWS_BYTES, at + 2 * _ROWS_BYTES,
+                 spd.data_ptr(), table.data_ptr(), table.shape[1], at + 3 * _ROWS_BYTES, lse.data_ptr(), T,
+                 _ptr(workspace), 0 if workspace is None else workspace.numel(), d, _dt(q), scale, cap, drop, s)
     _check(st, "gt_attn_pack_fwd")
     return out, lse
 
@@ -269,22 +299,25 @@ def gt_attn_pack_bwd(q, k, v, spd, table, pack: GTPack, o, lse, d_o, scale: floa
     """dQ, dK, dV and dTable of the packed batch (C ABI gt_attn_pack_bwd), with
     the forward's arguments and results. `grads` may hold preallocated (dq, dk,
     dv, dtable); rows behind the batch's totals stay as they are."""
-    dt, H, d, dev, (rq, rk, rv), scale, cap = _common(q, k, v, spd, table, pack, scale, cap)
+    dt, H, d, dev, rows, scale, cap = _common(q, k, v, spd, table, pack, scale, cap)
     T, nb = q.shape[1], table.shape[1]
-    drop = _dropout(dropout, dev)
-    ro, rdo = _rows(o, "o", H, pack.total_q, d, dt), _rows(d_o, "d_o", H, pack.total_q, d, dt)
+    drop = None if dropout is None else _dropout(dropout, dev)
     _lse(lse, H, T)
     made = []
     if grads is None:
         grads = made = [torch.empty(x.shape, device=q.device, dtype=x.dtype) for x in (q, k, v, table)]
-    _need(len(grads) == 4, "grads must be (dq, dk, dv, dtable)")
+    elif len(grads) != 4:
+        raise ValueError("grads must be (dq, dk, dv, dtable)")
     dq, dk, dv, dtable = grads
-    rdq = _rows(dq, "dq", H, pack.total_q, d, dt, written=True)
-    rdk = _rows(dk, "dk", H, pack.total_k, d, dt, written=True)
-    rdv = _rows(dv, "dv", H, pack.total_k, d, dt, written=True)
+    tq, tk = pack.total_q, pack.total_k
+    r = _Rows8(*rows, *_rows(o, "o", H, tq, d, dt, dev), *_rows(d_o, "d_o", H, tq, d, dt, dev),
+               *_rows(dq, "dq", H, tq, d, dt, dev, written=True), *_rows(dk, "dk", H, tk, d, dt, dev, written=True),
+               *_rows(dv, "dv", H, tk, d, dt, dev, written=True))
+    at = [ctypes.addressof(r) + i * _ROWS_BYTES for i in range(8)]
     _shape(dtable, "dtable", table.shape, torch.float32)
-    _need(dtable.is_contiguous(), "dtable must be contiguous")
-    _same_device(dev, o, lse, d_o, dq, dk, dv, dtable)
+    if not dtable.is_contiguous():
+        raise ValueError("dtable must be contiguous")
+    _same_device(dev, lse, dtable)
     need = gt_attn_pack_bwd_workspace_size(pack, nb)
     if workspace is not None:
         _workspace(workspace, need, q)
@@ -292,9 +325,8 @@ def gt_attn_pack_bwd(q, k, v, spd, table, pack: GTPack, o, lse, d_o, scale: floa
         workspace = torch.empty(need, device=q.device, dtype=torch.uint8)
         made = [*made, workspace]
     s = _on_stream(dev, stream, pack._plan, *made)
-    b = ctypes.byref
-    st = _launch(dev, lib().gt_attn_pack_bwd, b(pack._info), _ptr(pack._plan), b(rq), b(rk), b(rv), _ptr(spd),
-                 _ptr(table), nb, b(ro), _ptr(lse), T, b(rdo), b(rdq), b(rdk), b(rdv), _ptr(dtable),
-                 _ptr(workspace), workspace.numel(), d, _dt(q), scale, cap, drop, s)
+    st = _launch(dev, lib().gt_attn_pack_bwd, pack._at, pack._plan_at, at[0], at[1], at[2], spd.data_ptr(),
+                 table.data_ptr(), nb, at[3], lse.data_ptr(), T, at[4], at[5], at[6], at[7], dtable.data_ptr(),
+                 workspace.data_ptr(), workspace.numel(), d, _dt(q), scale, cap, drop, s)
     _check(st, "gt_attn_pack_bwd")
     return dq, dk, dv, dtable

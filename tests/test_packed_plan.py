@@ -186,7 +186,7 @@ BOTH = [(dict(info=False), 1), (dict(plan=None), 1), (dict(plan=MIS), 1), (dict(
         (dict(v=(FAKE, 2560, (1 << 23) + 8)), 1), (dict(spd=None), 1), (dict(table=None), 1), (dict(lse=None), 1),
         (dict(ld=39), 1), (dict(nb=0), 1), (dict(nb=257), 1), (dict(d=48), 2), (dict(d=128), 2), (dict(dtype=2), 2),
         (dict(scale=0.0), 1), (dict(scale=float("nan")), 1), (dict(cap=-1.0), 1), (dict(cap=float("inf")), 1),
-        (dict(cap=float("nan")), 1), (dict(p=-0.1), 1), (dict(p=1.0), 1), (dict(p=1 - 1e-6), 1),
+        (dict(cap=float("nan")), 1), (dict(cap=2.0 ** -11), 1), (dict(cap=1025.0), 1), (dict(p=-0.1), 1), (dict(p=1.0), 1), (dict(p=1 - 1e-6), 1),
         (dict(p=float("nan")), 1), (dict(p=0.1, offset_dev=0x10002), 1)]
 
 
