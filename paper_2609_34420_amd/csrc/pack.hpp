@@ -54,8 +54,8 @@ struct PackArgs {
   float* lse_part;          // [slot, H, 32]
   float* dlt;               // [H, ld_dlt] rowsum(dO * O)
   int64_t ld_dlt;
-  float2* dmax;             // [H, njobs_dq * 4] of each wave of the dQ kernel: largest |dS|, and
-                            // largest correction of a row's D
+  float2* dmax;             // [H, njobs_dq] of each job of the dQ kernel: largest |dS|, and largest
+                            // correction of a row's D
   int32_t njobs_dq;
   double* dtab_part;        // [H, slots, n_buckets]
   float* dtable;            // [H, n_buckets]

@@ -93,7 +93,7 @@ BwdParts bwd_parts(const gt_attn_pack_t* p, int32_t n_buckets) {
   const size_t H = (size_t)p->H;
   BwdParts b;
   b.dmax = pad256(H * (size_t)p->total_q * sizeof(float));
-  b.dtab = b.dmax + pad256(H * (size_t)p->jobs[1] * kPackWaves * sizeof(float2));
+  b.dtab = b.dmax + pad256(H * (size_t)p->jobs[1] * sizeof(float2));
   b.bytes = b.dtab + pad256(H * (size_t)p->slots * (size_t)n_buckets * sizeof(double));
   return b;
 }

@@ -78,12 +78,22 @@ __global__ __launch_bounds__(kPackThreads, M::D == 32 && M::BF16 ? 2 : (M::BF16 
   for (int t = tid; t < a.n_buckets * CPY / 2; t += kPackThreads)
     reinterpret_cast<uint4*>(hist)[t] = make_uint4(0u, 0u, 0u, 0u);
   {
-    const float2* dm = a.dmax + (int64_t)h * a.njobs_dq * kPackWaves;
+    // (four loads in flight: one after the other they took a third of a short
+    // workgroup's time)
+    const float2* dm = a.dmax + (int64_t)h * a.njobs_dq;
     float x = 0.0f, y = 0.0f;
-    for (int t = tid; t < a.njobs_dq * kPackWaves; t += kPackThreads) {
-      const float2 v = dm[t];
-      x = fmaxf(x, v.x);
-      y = fmaxf(y, v.y);
+    for (int t = tid; t < a.njobs_dq; t += 4 * kPackThreads) {
+      float2 v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int i = t + k * kPackThreads;
+        v[k] = dm[i < a.njobs_dq ? i : t];
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        x = fmaxf(x, v[k].x);
+        y = fmaxf(y, v[k].y);
+      }
     }
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) {
@@ -212,6 +222,13 @@ __global__ __launch_bounds__(kPackThreads, M::D == 32 && M::BF16 ? 2 : (M::BF16 
         dl[4 * u] = z.x; dl[4 * u + 1] = z.y; dl[4 * u + 2] = z.z; dl[4 * u + 3] = z.w;
       }
       bias16(sTab, b, x);
+      // (masks enter with the biases, so that the element work is one run of
+      // instructions: 3 % at d = 64; with dropout after the exponential, 5 % at d = 8)
+      if (!DROP && (i0 < lo1 || jw + 32 > gr.nk)) {
+        const int r0 = jok ? lo - i0 - 16 * g : 16;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[r] = r >= r0 ? x[r] : -INFINITY;
+      }
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         s[r] = START ? ml[r] : 0.0f;
@@ -230,7 +247,7 @@ __global__ __launch_bounds__(kPackThreads, M::D == 32 && M::BF16 ? 2 : (M::BF16 
       float p[16];
 #pragma unroll
       for (int r = 0; r < 16; ++r) p[r] = M::expo(x[r]);
-      if (i0 < lo1 || jw + 32 > gr.nk) {
+      if (DROP && (i0 < lo1 || jw + 32 > gr.nk)) {
         const int r0 = jok ? lo - i0 - 16 * g : 16;
 #pragma unroll
         for (int r = 0; r < 16; ++r) p[r] = r >= r0 ? p[r] : 0.0f;

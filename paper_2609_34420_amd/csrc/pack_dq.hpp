@@ -12,7 +12,7 @@
 // dK / dV kernel is D0 plus it, and dQ is corrected by it times the sum of
 // P (1 - tanh^2) K, which takes a second product per key tile.
 //
-// It also gives the largest |dS| of each wave and the largest correction of D,
+// It also gives the largest |dS| of each job and the largest correction of D,
 // from which the dK / dV kernel takes the scale of its fixed-point table gradient.
 #pragma once
 #include "pack.hpp"
@@ -32,6 +32,7 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_dq_kernel(PackArgs a) {
   __shared__ alignas(128) uint8_t sBuf0[STG > XCH ? STG : XCH];
   __shared__ alignas(128) uint8_t sBuf1[NB == 2 ? STG : 16];
   __shared__ float sTab[256];
+  __shared__ float2 sMax[kPackWaves];
   __shared__ uint4 sKeys[DROP ? NB * kPackWaves * 4 : 1];
 
   const PackPlace pl(a, a.njobs);
@@ -224,7 +225,6 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_dq_kernel(PackArgs a) {
   dsum = (dsum + __shfl_xor(dsum, 32)) * pm;
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) dmax = fmaxf(dmax, __shfl_xor(dmax, o));
-  float2* dm = a.dmax + ((int64_t)h * a.njobs + pl.job) * kPackWaves + wave;
   if (gr.combine) {
     float* stat = reinterpret_cast<float*>(sBuf0 + NA * 16 * 64 * 4 * 2) + lane;
     pack_combine(
@@ -236,28 +236,33 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_dq_kernel(PackArgs a) {
     if constexpr (FIX)
       pack_combine(reinterpret_cast<float*>(sBuf0), lw, grp, gw, fix, [](int) {},
                    [](int, float& wa, float& wo) { wa = wo = 1.0f; });
-    if (grp != 0) {
-      if (lane == 0) *dm = make_float2(dmax * rp, 0.0f);
-      return;
-    }
   }
-  float cmax = fabsf(dsum);
+  const bool mine = !gr.combine || grp == 0;             // the wave holds its rows' results
+  float cmax = mine ? fabsf(dsum) : 0.0f;
 #pragma unroll
   for (int o = 16; o >= 1; o >>= 1) cmax = fmaxf(cmax, __shfl_xor(cmax, o));
-  if (lane == 0) *dm = make_float2(dmax * rp, cmax * rp);
-  if (!iok) return;
-  const float mul = a.scale * rp * pm * (CAP ? M::kSlope : 1.0f);
-  if constexpr (FIX) {
+  if (lane == 0) sMax[wave] = make_float2(dmax, cmax);
+  if (mine && iok) {
+    const float mul = a.scale * rp * pm * (CAP ? M::kSlope : 1.0f);
+    if constexpr (FIX) {
 #pragma unroll
-    for (int c = 0; c < NA; ++c)
+      for (int c = 0; c < NA; ++c)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[c][r] = fmaf(-dsum, fix[c][r], acc[c][r]);
+        for (int r = 0; r < 16; ++r) acc[c][r] = fmaf(-dsum, fix[c][r], acc[c][r]);
+    }
+    T* out = rows_at<T>(a.dq, h, gr.q0 + i);
+    M::features(acc, [&](int f, float4 v) {
+      M::store4(out + f, make_float4(v.x * mul, v.y * mul, v.z * mul, v.w * mul));
+    });
+    if (g == 0) a.dlt[h * a.ld_dlt + gr.q0 + i] = dlt + dsum;    // D (1 - p)
   }
-  T* out = rows_at<T>(a.dq, h, gr.q0 + i);
-  M::features(acc, [&](int f, float4 v) {
-    M::store4(out + f, make_float4(v.x * mul, v.y * mul, v.z * mul, v.w * mul));
-  });
-  if (g == 0) a.dlt[h * a.ld_dlt + gr.q0 + i] = dlt + dsum;      // D (1 - p)
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    float2 m = sMax[0];
+#pragma unroll
+    for (int k = 1; k < kPackWaves; ++k) m = make_float2(fmaxf(m.x, sMax[k].x), fmaxf(m.y, sMax[k].y));
+    a.dmax[(int64_t)h * a.njobs + pl.job] = make_float2(m.x * rp, m.y * rp);
+  }
 }
 
 template <class M>
