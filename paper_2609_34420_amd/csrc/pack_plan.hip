@@ -22,7 +22,6 @@ namespace {
 
 constexpr int64_t kMaxNodes = (1LL << 25) - 16;   // 32 rows of distances stay below 2^31 bytes
 constexpr int kSlots = 512;                       // workgroups that run at a time: two per compute unit
-constexpr int kSetup = 3;                         // cost of a workgroup's start and end, in 32 x 32 blocks
 
 enum Stage { kForward, kDq, kDkdv };
 
@@ -38,6 +37,7 @@ struct Group {
 struct Job {
   int32_t group;       // first of its 4 / W groups
   int32_t log2w, combine, steps;
+  int32_t cost;        // 32 x 32 blocks of its longest wave
 };
 
 struct Plan {
@@ -71,7 +71,6 @@ struct Item {
 Plan build(const std::vector<Graph>& graphs, int32_t H, Stage st, int s) {
   Plan p;
   std::vector<std::vector<Item>> whole(3);         // by log2w: groups that share a workgroup with others
-  std::vector<std::pair<int32_t, Job>> jobs;       // cost, job
   std::vector<std::pair<Item, int>> split;         // combined: item, log2w
   for (size_t gi = 0; gi < graphs.size(); ++gi) {
     const Graph& g = graphs[gi];
@@ -94,10 +93,10 @@ Plan build(const std::vector<Graph>& graphs, int32_t H, Stage st, int s) {
     std::stable_sort(w.begin(), w.end(), [](const Item& a, const Item& b) { return a.cost > b.cost; });
     const int n = kPackWaves >> lw;
     for (size_t i = 0; i < w.size(); i += n) {
-      const Job j{(int32_t)p.groups.size(), lw, 0, (w[i].cost + (1 << lw) - 1) >> lw};
+      const Job j{(int32_t)p.groups.size(), lw, 0, (w[i].cost + (1 << lw) - 1) >> lw, w[i].cost};
       for (int k = 0; k < n; ++k)
         p.groups.push_back(i + k < w.size() ? w[i + k].g : Group{-1, 0, 0, 0, -1});
-      jobs.push_back({w[i].cost, j});
+      p.jobs.push_back(j);
     }
   }
   // Parts: with 32-row workgroups that still leave the chip empty, as many per
@@ -131,7 +130,7 @@ Plan build(const std::vector<Graph>& graphs, int32_t H, Stage st, int s) {
     for (int32_t k = 0; k < parts; ++k) {
       const int32_t a = it.g.c0 + k * per_part, b = parts == 1 ? it.g.c1 : std::min(it.g.c1, a + per_part);
       const int32_t per = ((b - a + n - 1) / n + (32 << lw) - 1) / (32 << lw) * (32 << lw);
-      const Job j{(int32_t)p.groups.size(), lw, n > 1 ? 1 : 0, per / (32 << lw)};
+      const Job j{(int32_t)p.groups.size(), lw, n > 1 ? 1 : 0, per / (32 << lw), per / 32};
       for (int i = 0; i < n; ++i) {
         Group g = it.g;
         g.c0 = (int32_t)std::min<int64_t>(a + (int64_t)i * per, b > a ? (b + 31) / 32 * 32 : a);
@@ -140,12 +139,10 @@ Plan build(const std::vector<Graph>& graphs, int32_t H, Stage st, int s) {
         p.groups.push_back(g);
       }
       if (parts > 1) ++p.parts;
-      jobs.push_back({per / 32, j});
+      p.jobs.push_back(j);
     }
   }
-  std::stable_sort(jobs.begin(), jobs.end(),
-                   [](const std::pair<int32_t, Job>& a, const std::pair<int32_t, Job>& b) { return a.first > b.first; });
-  for (auto& j : jobs) p.jobs.push_back(j.second);
+  std::stable_sort(p.jobs.begin(), p.jobs.end(), [](const Job& a, const Job& b) { return a.cost > b.cost; });
   return p;
 }
 
@@ -162,24 +159,33 @@ std::vector<PackWave> waves(const std::vector<Graph>& graphs, const Plan& p) {
   return out;
 }
 
-// The longest workgroup, or the chip's share of all of them.
-double span(const Plan& p, int32_t H) {
+// How long a plan takes, in 32 x 32 blocks of a workgroup alone on its compute unit:
+// its longest workgroup, or the work over what the chip does with two on every unit
+// (1.4 times one; each then runs at 0.7). Sharing rows between groups of waves costs
+// more copies and barriers per block (1, 1.05 and 1.2 with 1, 2 and 4 groups) and
+// the addition of their results. Forward and backward over 20 batches of 500 to
+// 16384 nodes, bf16 and fp32, head dims 16 to 64: within 5 % of the best of the three
+// nearly everywhere (7651 nodes, d = 64, bf16, backward: 888 / 947 / 1099 us with 1 / 2 /
+// 4; 1000 nodes 99 / 64 / 49; 16 graphs of 300: 59 / 71 / 80).
+double span(const Plan& p, int32_t H, int s) {
+  const double per_block = s == 1 ? 1.0 : (s == 2 ? 1.05 : 1.2);
   double sum = 0.0, top = 0.0;
   for (const Job& j : p.jobs) {
-    const double c = (double)j.steps * (1 << j.log2w) + kSetup;
+    const double c = j.cost * per_block + (j.combine ? 5.0 : 3.0);
     sum += c;
     top = std::max(top, c);
   }
-  return std::max(sum * H / kSlots, top) + (p.parts ? 8.0 : 0.0);
+  const double wgs = (double)p.jobs.size() * H;
+  return std::max(sum * H / (256 * 1.4), wgs <= 256.0 ? top : top / 0.7) + (p.parts ? 8.0 : 0.0);
 }
 
 Plan best_plan(const std::vector<Graph>& graphs, int32_t H, Stage st) {
   Plan best = build(graphs, H, st, 1);
-  double cost = span(best, H);
+  double cost = span(best, H, 1);
   for (int s = 2; s <= 4; s *= 2) {
     Plan p = build(graphs, H, st, s);
-    const double c = span(p, H);
-    if (c < 0.95 * cost) {
+    const double c = span(p, H, s);
+    if (c < 0.97 * cost) {
       cost = c;
       best = std::move(p);
     }
@@ -194,7 +200,7 @@ Plan best_plan(const std::vector<Graph>& graphs, int32_t H, Stage st) {
 int32_t slots(const Plan& p, int32_t H) {
   const int64_t n = (int64_t)p.jobs.size();
   int64_t sum = 0;
-  for (const Job& j : p.jobs) sum += (int64_t)j.steps << j.log2w;
+  for (const Job& j : p.jobs) sum += j.cost;
   const int64_t by_work = (sum + 15) / 16;
   const int64_t full = (kSlots + H - 1) / H;
   return (int32_t)std::min(n, std::max(by_work, full));
