@@ -16,26 +16,33 @@ __global__ __launch_bounds__(256) void pack_merge_kernel(PackArgs a, int d) {
   for (int t = threadIdx.x; t < mg.rows * cpr; t += 256) {
     const int row = t / cpr, f = t % cpr * 4;
     const auto at = [&](int p) { return ((int64_t)(mg.part + p) * a.H + h) * 32 + row; };
-    float m = -INFINITY;
-    for (int p = 0; p < mg.parts; ++p) {
-      const float l = a.lse_part[at(p)];
-      m = l > m || isnan(l) ? l : m;
-    }
+    // one pass with a running maximum, 8 parts' loads in flight
+    float m = -INFINITY, tot = 0.0f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int p0 = 0; p0 < mg.parts; p0 += 8) {
+      float l[8];
+      float4 v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int64_t x = at(p0 + k < mg.parts ? p0 + k : p0);
+        l[k] = a.lse_part[x];
+        v[k] = *reinterpret_cast<const float4*>(a.o_part + x * d + f);
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        if (p0 + k >= mg.parts || l[k] == -INFINITY) continue;
+        const float mn = l[k] > m || isnan(l[k]) ? l[k] : m;
+        const float wo = m == -INFINITY ? 0.0f : expf(m - mn), w = expf(l[k] - mn);
+        m = mn;
+        tot = fmaf(tot, wo, w);
+        o.x = fmaf(o.x, wo, w * v[k].x);
+        o.y = fmaf(o.y, wo, w * v[k].y);
+        o.z = fmaf(o.z, wo, w * v[k].z);
+        o.w = fmaf(o.w, wo, w * v[k].w);
+      }
+    }
     float lse = -INFINITY;
     if (m != -INFINITY) {
-      float tot = 0.0f;
-      for (int p = 0; p < mg.parts; ++p) {
-        const float lp = a.lse_part[at(p)];
-        if (lp == -INFINITY) continue;
-        const float w = expf(lp - m);
-        const float4 v = *reinterpret_cast<const float4*>(a.o_part + at(p) * d + f);
-        tot += w;
-        o.x = fmaf(w, v.x, o.x);
-        o.y = fmaf(w, v.y, o.y);
-        o.z = fmaf(w, v.z, o.z);
-        o.w = fmaf(w, v.w, o.w);
-      }
       const float inv = 1.0f / tot;
       o.x *= inv; o.y *= inv; o.z *= inv; o.w *= inv;
       lse = m + logf(tot);
@@ -55,8 +62,14 @@ __global__ __launch_bounds__(256) void pack_dtable_kernel(PackArgs a) {
   const int h = blockIdx.y, b = blockIdx.x * 16 + threadIdx.x % 16;
   double s = 0.0;
   if (b < a.n_buckets)
-    for (int j = threadIdx.x / 16; j < a.slots; j += 16)
-      s += a.dtab_part[((int64_t)h * a.slots + j) * a.n_buckets + b];
+    for (int j = threadIdx.x / 16; j < a.slots; j += 16 * 8) {
+      double v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        v[k] = j + 16 * k < a.slots ? a.dtab_part[((int64_t)h * a.slots + j + 16 * k) * a.n_buckets + b] : 0.0;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s += v[k];
+    }
   red[threadIdx.x] = s;
   __syncthreads();
   if (threadIdx.x < 16 && b < a.n_buckets) {
