@@ -138,6 +138,26 @@ def test_bucket_counts(dt, nb):
     check(f"buckets {dt} nb={nb}", [150, 40], 2, 16, nb, dt, cap=8.0)
 
 
+@pytest.mark.parametrize("drop", [None, gt.GTDropout(0.1, 21, 5)])
+def test_table_gradient_of_many_pairs(drop):
+    """The table gradient sums some millions of terms of either sign: roundings that
+    lean to one side would show. Uncapped scores of up to 20 are 29 in base 2, rounded
+    twice: P is off by up to 2 * 29 * 2^-24 ln 2 = 2.4e-6, twice that with the LSE's."""
+    n, H, d, nb = [2500], 2, 8, 20
+    a = make(n, n, H, d, nb, "bf16", seed=31)
+    r = upload(a)
+    pack = gt.gt_attn_pack(n, H, device=DEV)
+    args = (r["q"], r["k"], r["v"], r["spd"], r["table"], pack)
+    o, lse = gt.gt_attn_pack_fwd(*args, dropout=drop)
+    got = gt.gt_attn_pack_bwd(*args, o, lse, r["do"], dropout=drop)[3]
+    torch.cuda.synchronize()
+    want = oracle.packed_backward(a["q"], a["k"], a["v"], a["spd"], a["table"], d ** -0.5, a["do"], n, n,
+                                  dropout=drop and (drop.p, drop.seed, drop.offset))[3]
+    e = rel_l2(to_np(got), want)
+    say(f"table gradient of 2500 nodes: {e:.2e}")
+    assert e <= 5e-6
+
+
 def test_many_small_graphs():
     g = np.random.default_rng(5)
     check("many small", [int(x) for x in g.integers(1, 50, 300)], 4, 8, 22, "bf16", cap=20.0, drop=DROP)
