@@ -346,7 +346,8 @@ gt_status_t gt_attn_bwd_ring_step(const void* q_shard, const void* o_shard,
  *   without a prefix: all; with prefix[g]: those with j < prefix[g] or
  *   j <= i + n_k[g] - n_q[g] (the last query stands at the last key; prefix 0
  *   is the causal mask).
- * Table entries of -1e30 and less are masks, as -inf is. A row that sees no key,
+ * Table entries of -6e4 and less (the lowest fp16 and bf16 numbers too) are masks, as
+ * -inf is. A row that sees no key,
  * or only masked ones, gets O = 0, LSE = -inf and zero gradient. LSE counts
  * dropped pairs. V of a key that a row does not see, or only behind a mask,
  * does not reach the row unless it is NaN or infinite (within one graph 0 times
@@ -364,7 +365,8 @@ gt_status_t gt_attn_bwd_ring_step(const void* q_shard, const void* o_shard,
  * Tensors of rows: element (h, row, c) at p + h head_stride + row row_stride + c,
  * strides in elements, so [H, rows, d] and [rows, H, d] layouts are taken as they
  * are. p 16-byte aligned, strides multiples of 16 bytes, row_stride from d to
- * 2^23. Rows from the batch's total on are neither read nor written. */
+ * 2^23; the rows of a written tensor do not overlap. Rows from the batch's total on are
+ * neither read nor written. A captured graph reads the plan at each replay. */
 typedef struct {
   void* p;
   int64_t head_stride, row_stride;
@@ -400,7 +402,8 @@ typedef struct {
  *   plan      NULL: only *info is filled; else host memory of plan_bytes bytes that
  *             receives the plan, which the caller copies to device memory (16-byte
  *             aligned) and passes to the calls as it is.
- * GT_ERR_WORKSPACE: plan_bytes is below info->plan_bytes (*info is filled), or no
+ * GT_ERR_UNSUPPORTED: a size is above its limit, 2^31 rows or more in all, or more than
+ * about 2^24 workgroups. GT_ERR_WORKSPACE: plan_bytes is below info->plan_bytes (*info is filled), or no
  * host memory. All arrays are HOST arrays. */
 gt_status_t gt_attn_pack_plan(int32_t n_graphs, int32_t H, const int32_t* n_q, const int32_t* n_k,
                               const int32_t* prefix, const int64_t* spd_off, const int64_t* spd_ld,
@@ -416,6 +419,7 @@ size_t gt_attn_pack_bwd_workspace_size(const gt_attn_pack_t* pack, int32_t n_buc
  *   q [H, >= total_q, d], k, v [H, >= total_k, d] dtype; o as q (written)
  *   spd    >= pack->spd_bytes bytes    table [H, n_buckets] fp32
  *   lse    [H, ld_lse] fp32 (written), ld_lse >= total_q
+ *   scale  2^-64 .. 2^64
  *   cap    0 (no cap), or in 2^-10 .. 2^10 (scores are off by up to about 2^-21 cap)
  *   dropout NULL: none
  * Otherwise as gt_attn_fwd. Deterministic. */

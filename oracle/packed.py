@@ -63,7 +63,7 @@ def _probabilities(q, k, spd, table_h, scale, cap, prefix):
     u = scale * (q @ k.T)
     t = np.tanh(u / cap) if cap else None
     tab = np.asarray(table_h, dtype=np.float64)
-    S = (cap * t if cap else u) + bias_block(spd, np.where(tab <= -1e30, -np.inf, tab))
+    S = (cap * t if cap else u) + bias_block(spd, np.where(tab <= -6e4, -np.inf, tab))
     if prefix is not None:
         i, j = np.arange(nq)[:, None], np.arange(nk)[None]
         S = np.where((j < prefix) | (j <= i + nk - nq), S, -np.inf)

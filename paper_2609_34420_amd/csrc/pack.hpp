@@ -66,7 +66,10 @@ namespace {
 typedef short s16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kPackThreads = kPackWaves * 64;
-constexpr float kNoScore = -1e30f;        // table entries at or below it are masks, as -inf
+// Table entries at or below it are masks, as -inf. The backward takes P from the
+// log-sum-exp, whose last bit grows with it: of a row whose entries are all near
+// -6e4, P is off by 0.4 %, near -1e9 it would be off by powers of e^64.
+constexpr float kNoScore = -6e4f;
 
 // Wave-uniform values that the compiler took for divergent (a buffer resource of
 // such is read lane by lane).

@@ -10,6 +10,8 @@ namespace {
 
 constexpr int64_t kMaxRowStride = 1LL << 23;     // 32 rows of a tile stay below 2^30 bytes
 constexpr float kMinCap = 1.0f / 1024, kMaxCap = 1024.0f;
+// Products of scale, its inverse, caps and biases stay finite.
+constexpr float kMinScale = 0x1p-64f, kMaxScale = 0x1p64f;
 
 inline size_t pad256(size_t x) { return (x + 255) / 256 * 256; }
 inline bool aligned(const void* p, unsigned n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
@@ -39,7 +41,7 @@ gt_status_t common(const gt_attn_pack_t* pack, const void* plan, const gt_attn_r
   if (dtype != GT_F32 && dtype != GT_BF16) return GT_ERR_UNSUPPORTED;
   if (d != 8 && d != 16 && d != 32 && d != 64) return GT_ERR_UNSUPPORTED;
   if (!pack_ok(pack)) return GT_ERR_INVALID;
-  if (n_buckets < 1 || n_buckets > 256 || !std::isfinite(scale) || !(scale > 0.0f)) return GT_ERR_INVALID;
+  if (n_buckets < 1 || n_buckets > 256 || !(scale >= kMinScale && scale <= kMaxScale)) return GT_ERR_INVALID;
   if (cap != 0.0f && !(cap >= kMinCap && cap <= kMaxCap)) return GT_ERR_INVALID;
   if (!rows_ok(q, pack->total_q, d, dtype) || !rows_ok(o, pack->total_q, d, dtype) ||
       !rows_ok(k, pack->total_k, d, dtype) || !rows_ok(v, pack->total_k, d, dtype))

@@ -131,7 +131,7 @@ __global__ __launch_bounds__(kPackThreads, M::D == 32 && M::BF16 ? 2 : (M::BF16 
     int e;
     frexpf(bound, &e);                                    // bound < 2^e
     fexp = 30 - e;
-    fexp = fexp > 60 ? 60 : (fexp < -60 ? -60 : fexp);
+    fexp = fexp < 90 ? fexp : 90;                         // (at least -98; V 2^F is finite up to 2^37)
   }
   const float sF = ldexpf(1.0f, fexp);
 

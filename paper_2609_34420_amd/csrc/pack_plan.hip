@@ -251,7 +251,9 @@ gt_status_t make(int32_t G, int32_t H, const int32_t* n_q, const int32_t* n_k, c
   const Stage stages[3] = {kForward, kDq, kDkdv};
   for (int i = 0; i < 3; ++i) {
     const Plan p = best_plan(graphs, H, stages[i]);
-    if (((int64_t)p.jobs.size() + 8) * H > std::numeric_limits<int32_t>::max()) return GT_ERR_UNSUPPORTED;
+    // (a launch counts its threads in 32 bits)
+    if (((int64_t)p.jobs.size() + 8) * H * kPackWaves * 64 > std::numeric_limits<uint32_t>::max())
+      return GT_ERR_UNSUPPORTED;
     lists[i] = waves(graphs, p);
     info.jobs[i] = (int32_t)p.jobs.size();
     if (i == kForward) {

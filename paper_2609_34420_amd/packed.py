@@ -108,7 +108,8 @@ def gt_attn_pack(n_q, H: int, n_k=None, prefix=None, spd_off=None, spd_ld=None, 
     number of leading keys that every row of a graph sees beside those up to its own
     position (0: causal). spd_off, spd_ld: where a graph's distances lie in spd and
     their row stride, where they are not dense, one matrix behind the other. Made
-    once per batch of sizes, it serves every layer's and step's calls."""
+    once per batch of sizes, it serves every layer's and step's calls; a captured
+    graph reads it at each replay, so it has to live as long."""
     nq = _sizes(n_q, "n_q", None)
     nk = nq if n_k is None else _sizes(n_k, "n_k", nq.size)
     opt = [None if x is None else _sizes(x, name, nq.size, t)
@@ -177,7 +178,8 @@ def _rows(t, name: str, H: int, rows: int, d: int, dtype, dev: int, written: boo
 
 
 def _dropout(dropout, dev: int):
-    if dropout is None or dropout.p == 0:
+    _need(isinstance(dropout, GTDropout), "dropout must be a GTDropout or None")
+    if dropout.p == 0:
         return None
     p, seed, offset, dyn = dropout
     _need(0.0 <= p < 1.0 and round(p * 65536) <= 65535, f"dropout must lie in 0 <= p < 1 - 2^-17, got {p}")

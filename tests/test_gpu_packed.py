@@ -163,13 +163,14 @@ def test_many_small_graphs():
     check("many small", [int(x) for x in g.integers(1, 50, 300)], 4, 8, 22, "bf16", cap=20.0, drop=DROP)
 
 
+@pytest.mark.parametrize("mask", [-1e9, float(np.finfo(np.float16).min)])
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
-def test_masked_entries_and_empty_rows(dt):
-    """Table masks (-inf, and the type's lowest value, which counts as one),
-    with rows that they leave nothing."""
+def test_masked_entries_and_empty_rows(dt, mask):
+    """Table masks (-inf, and large negative values, which count as one: the lowest
+    of fp32 and of fp16, and -1e9), with rows that they leave nothing."""
     n = [70, 40]
     a = make(n, n, 2, 32, 10, dt, seed=4)
-    a["table"][:, 3], a["table"][:, 4], a["table"][:, 5] = -np.inf, np.finfo(np.float32).min, -1e30
+    a["table"][:, 3], a["table"][:, 4], a["table"][:, 5] = -np.inf, np.finfo(np.float32).min, mask
     for base, w in ((0, 70), (70 * 70, 40)):
         a["spd"][base + 7 * w:base + 8 * w] = 3 + np.arange(w) % 3        # row 7 of each graph
     r = upload(a)
@@ -305,6 +306,51 @@ def test_rows_behind_the_batch_and_layouts():
     ref = gt.gt_attn_pack_fwd(r["q"], shared.contiguous(), r["v"], r["spd"], r["table"], pack)
     torch.cuda.synchronize()
     assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("cap,drop", [(None, None), (7.0, DROP)])
+def test_gradients_scale_with_d_o(dt, cap, drop):
+    """d_o times a power of two: every gradient times it, bit by bit (nothing
+    of the fixed-point sums or the staged values leaves its range)."""
+    n, H = [150, 40], 2
+    r = upload(make(n, n, H, 32, 22, dt, seed=14))
+    pack = gt.gt_attn_pack(n, H, device=DEV)
+    args = (r["q"], r["k"], r["v"], r["spd"], r["table"], pack)
+    o, lse = gt.gt_attn_pack_fwd(*args, cap=cap, dropout=drop)
+    want = gt.gt_attn_pack_bwd(*args, o, lse, r["do"], cap=cap, dropout=drop)
+    for e in (-50, -25, 35, 60):
+        got = gt.gt_attn_pack_bwd(*args, o, lse, r["do"] * 2.0 ** e, cap=cap, dropout=drop)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y * 2.0 ** e) for x, y in zip(got, want)), e
+
+
+def test_offsets_past_32_bits():
+    """Rows 2^23 elements apart, so that the last ones lie past 2^32 elements, in
+    one buffer for all tensors; distances past 5 GiB; against dense tensors."""
+    n, H, d, rs = [400, 150], 2, 32, 1 << 23
+    r = upload(make(n, n, H, d, 22, "bf16", seed=15))
+    pack = gt.gt_attn_pack(n, H, device=DEV)
+    args = (r["q"], r["k"], r["v"], r["spd"], r["table"], pack)
+    want = gt.gt_attn_pack_fwd(*args, cap=9.0)
+    want = (*want, *gt.gt_attn_pack_bwd(*args, *want, r["do"], cap=9.0))
+    T = sum(n)
+    buf = torch.empty(T * rs, device=DEV, dtype=torch.bfloat16)
+    q, k, v, do, o, dq, dk, dv = (buf.as_strided((H, T, d), (d, rs, 1), i * 1024) for i in range(8))
+    for x, y in ((q, "q"), (k, "k"), (v, "v"), (do, "do")):
+        x.copy_(r[y])
+    off = [5 << 30, 17]
+    spd = torch.empty(off[0] + n[0] * n[0], device=DEV, dtype=torch.uint8)
+    spd[off[0]:] = r["spd"][:n[0] * n[0]]
+    spd[off[1]:off[1] + n[1] * n[1]] = r["spd"][n[0] * n[0]:]
+    pack = gt.gt_attn_pack(n, H, spd_off=off, device=DEV)
+    args = (q, k, v, spd, r["table"], pack)
+    lse = torch.empty_like(want[1])
+    gt.gt_attn_pack_fwd(*args, cap=9.0, out=o, lse=lse)
+    dt = torch.empty_like(r["table"])
+    gt.gt_attn_pack_bwd(*args, o, lse, do, cap=9.0, grads=(dq, dk, dv, dt))
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip((o, lse, dq, dk, dv, dt), want))
 
 
 def test_empty_batches():

@@ -130,7 +130,8 @@ def test_plan_refusals():
         with pytest.raises(ValueError, match=what):
             gt.gt_attn_pack(**{**ok, **bad})
     for bad, code in [(dict(spd_ld=[2, 4]), 1), (dict(n_q=[1 << 25, 1]), 2), (dict(spd_ld=[1 << 25, 4]), 2),
-                      (dict(spd_off=[0, (1 << 63) - 5]), 1)]:
+                      (dict(spd_off=[0, (1 << 63) - 5]), 1),
+                      (dict(n_q=[128 * 260, 1], H=65535), 2)]:                   # 2^24 workgroups
         with pytest.raises(gt.GTError) as e:
             gt.gt_attn_pack(**{**ok, **bad})
         assert e.value.status == code, bad
@@ -185,7 +186,7 @@ BOTH = [(dict(info=False), 1), (dict(plan=None), 1), (dict(plan=MIS), 1), (dict(
         (dict(q=(FAKE, 2560, 68)), 1), (dict(k=(FAKE, 2564, 64)), 1), (dict(k=(FAKE, -2560, 64)), 1),
         (dict(v=(FAKE, 2560, (1 << 23) + 8)), 1), (dict(spd=None), 1), (dict(table=None), 1), (dict(lse=None), 1),
         (dict(ld=39), 1), (dict(nb=0), 1), (dict(nb=257), 1), (dict(d=48), 2), (dict(d=128), 2), (dict(dtype=2), 2),
-        (dict(scale=0.0), 1), (dict(scale=float("nan")), 1), (dict(cap=-1.0), 1), (dict(cap=float("inf")), 1),
+        (dict(scale=0.0), 1), (dict(scale=float("nan")), 1), (dict(scale=2.0 ** -65), 1), (dict(scale=2.0 ** 65), 1), (dict(cap=-1.0), 1), (dict(cap=float("inf")), 1),
         (dict(cap=float("nan")), 1), (dict(cap=2.0 ** -11), 1), (dict(cap=1025.0), 1), (dict(p=-0.1), 1), (dict(p=1.0), 1), (dict(p=1 - 1e-6), 1),
         (dict(p=float("nan")), 1), (dict(p=0.1, offset_dev=0x10002), 1)]
 
@@ -239,3 +240,14 @@ def test_binding_reaches_the_device_check():
 def test_binding_refusals(kw, what):
     with pytest.raises(ValueError, match=what):
         gt.gt_attn_pack_fwd(**args(**kw))
+
+
+@pytest.mark.parametrize("drop,what", [
+    (0.1, "GTDropout"), ((0.1, 3), "GTDropout"), (gt.GTDropout(1.0, 3), "dropout"), (gt.GTDropout(-0.1, 3), "dropout"),
+    (gt.GTDropout(float("nan"), 3), "dropout"), (gt.GTDropout(0.1, -1), "seed"), (gt.GTDropout(0.1, 1 << 64), "seed"),
+    (gt.GTDropout(0.1, 3, 1 << 32), "offset"), (gt.GTDropout(0.1, 3, -1), "offset"),
+    (gt.GTDropout(0.1, 3, 0, torch.zeros(1, dtype=torch.int32)), "offset_dev")])
+def test_dropout_refusals(drop, what):
+    with pytest.raises(ValueError, match=what):
+        gt.packed._dropout(drop, 0)
+    assert gt.packed._dropout(gt.GTDropout(0.0, 3), 0) is None
