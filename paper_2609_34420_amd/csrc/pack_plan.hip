@@ -3,9 +3,11 @@
 // prefixes and the number of heads.
 //
 // Rows are dealt out in blocks of 32 per wave. Where the batch fills the chip, a
-// graph of more than 64 rows gives workgroups of 128 rows, and smaller ones
-// share a workgroup, 2 or 4 of them (those with the most alike numbers of
-// columns together, since a workgroup's waves meet at every tile). Where it does
+// graph gives workgroups of 128 rows, and remainders of up to 64 rows (small graphs
+// are nothing else) share a workgroup, 2 or 4 of them, those with the most alike
+// numbers of columns together, since a workgroup's waves meet at every tile (512
+// graphs of 100 to 256 nodes, d = 8, with their remainders in workgroups of their own:
+// forward 80 us and 71 so, dQ 103 and 91, dK / dV 182 and 157). Where it does
 // not, 2 or 4 groups of waves take the same rows and a part of the columns each,
 // and in the forward with few rows against many keys several workgroups do, whose
 // partial results are merged by a kernel of its own.
@@ -75,12 +77,13 @@ Plan build(const std::vector<Graph>& graphs, int32_t H, Stage st, int s) {
   for (size_t gi = 0; gi < graphs.size(); ++gi) {
     const Graph& g = graphs[gi];
     const int32_t rows = st == kDkdv ? g.nk : g.nq;
-    int lw = s == 1 ? 2 : (s == 2 ? 1 : 0);
-    while (lw > 0 && rows <= (32 << (lw - 1))) --lw;
-    const int32_t step = 32 << lw;
-    for (int64_t r = 0; r < rows; r += step) {
-      Item it{{(int32_t)gi, (int32_t)r, 0, 0, -1}, 0};
-      columns(g, st, (int32_t)r, step, it.g.c0, it.g.c1);
+    int32_t step;
+    for (int32_t r = 0; r < rows; r += step) {
+      int lw = s == 1 ? 2 : (s == 2 ? 1 : 0);
+      while (lw > 0 && rows - r <= (32 << (lw - 1))) --lw;
+      step = 32 << lw;
+      Item it{{(int32_t)gi, r, 0, 0, -1}, 0};
+      columns(g, st, r, step, it.g.c0, it.g.c1);
       it.cost = (it.g.c1 - it.g.c0 + 31) / 32;
       if (s == 1)
         whole[lw].push_back(it);
@@ -161,13 +164,15 @@ std::vector<PackWave> waves(const std::vector<Graph>& graphs, const Plan& p) {
 
 // How long a plan takes, in 32 x 32 blocks of a workgroup alone on its compute unit:
 // its longest workgroup, or the work over what the chip does with two on every unit
-// (1.4 times one; each then runs at 0.7). Sharing rows between groups of waves costs
+// (1.4 times one; each then runs at 0.7, and in the forward, of which a unit takes
+// four, at 0.53: 16 causal graphs of up to 2400 nodes 85 us unsplit, 71 with two
+// groups). Sharing rows between groups of waves costs
 // more copies and barriers per block (1, 1.05 and 1.2 with 1, 2 and 4 groups) and
 // the addition of their results. Forward and backward over 20 batches of 500 to
 // 16384 nodes, bf16 and fp32, head dims 16 to 64: within 5 % of the best of the three
 // nearly everywhere (7651 nodes, d = 64, bf16, backward: 888 / 947 / 1099 us with 1 / 2 /
 // 4; 1000 nodes 99 / 64 / 49; 16 graphs of 300: 59 / 71 / 80).
-double span(const Plan& p, int32_t H, int s) {
+double span(const Plan& p, int32_t H, Stage st, int s) {
   const double per_block = s == 1 ? 1.0 : (s == 2 ? 1.05 : 1.2);
   double sum = 0.0, top = 0.0;
   for (const Job& j : p.jobs) {
@@ -176,15 +181,17 @@ double span(const Plan& p, int32_t H, int s) {
     top = std::max(top, c);
   }
   const double wgs = (double)p.jobs.size() * H;
-  return std::max(sum * H / (256 * 1.4), wgs <= 256.0 ? top : top / 0.7) + (p.parts ? 8.0 : 0.0);
+  double slower = wgs <= 256.0 ? 1.0 : 1 / 0.7;
+  if (st == kForward && wgs > 512.0) slower += 0.235 * (std::min(wgs / 256, 4.0) - 2.0);
+  return std::max(sum * H / (256 * 1.4), top * slower) + (p.parts ? 8.0 : 0.0);
 }
 
 Plan best_plan(const std::vector<Graph>& graphs, int32_t H, Stage st) {
   Plan best = build(graphs, H, st, 1);
-  double cost = span(best, H, 1);
+  double cost = span(best, H, st, 1);
   for (int s = 2; s <= 4; s *= 2) {
     Plan p = build(graphs, H, st, s);
-    const double c = span(p, H, s);
+    const double c = span(p, H, st, s);
     if (c < 0.97 * cost) {
       cost = c;
       best = std::move(p);
