@@ -191,7 +191,7 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_dq_kernel(PackArgs a) {
         put_keys(t0 + step, 1);
       }
       blocks(sK0, sV0, 0, t0);
-      t0 += step;
+      t0 = uniform(t0 + step);
       if (t + 1 >= gr.steps) break;
       wait_vmcnt<0>();
       lds_barrier();
@@ -200,7 +200,7 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_dq_kernel(PackArgs a) {
         put_keys(t0 + step, 0);
       }
       blocks(sK1, sV1, 1, t0);
-      t0 += step;
+      t0 = uniform(t0 + step);
     }
   } else {
     PackStage<M> tk, tv;

@@ -179,32 +179,32 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_fwd_kernel(PackArgs a) {
         lds_barrier();                                 // the tile has landed
         blocks(sK0, sV0, 0, t0);
       }
-      t0 = 0;
-    }
-    T* const sK1 = reinterpret_cast<T*>(sBuf1);
-    T* const sV1 = sK1 + (NB == 2 ? kPackWaves * M::TILE : 0);
-    if (NB == 2 && gr.steps > 0) {
-      copy(sK0, sV0, t0);
-      put_keys(t0, 0);
-    }
-    for (int t = 0; NB == 2 && t < gr.steps; t += 2) {
-      wait_vmcnt<0>();
-      lds_barrier();                                   // the tile has landed, the last one's reads are done
-      if (t + 1 < gr.steps) {
-        copy(sK1, sV1, t0 + step);
-        put_keys(t0 + step, 1);
+    } else {
+      T* const sK1 = reinterpret_cast<T*>(sBuf1);
+      T* const sV1 = sK1 + kPackWaves * M::TILE;
+      if (gr.steps > 0) {
+        copy(sK0, sV0, t0);
+        put_keys(t0, 0);
       }
-      blocks(sK0, sV0, 0, t0);
-      t0 += step;
-      if (t + 1 >= gr.steps) break;
-      wait_vmcnt<0>();
-      lds_barrier();
-      if (t + 2 < gr.steps) {
-        copy(sK0, sV0, t0 + step);
-        put_keys(t0 + step, 0);
+      for (int t = 0; t < gr.steps; t += 2) {
+        wait_vmcnt<0>();
+        lds_barrier();                                 // the tile has landed, the last one's reads are done
+        if (t + 1 < gr.steps) {
+          copy(sK1, sV1, t0 + step);
+          put_keys(t0 + step, 1);
+        }
+        blocks(sK0, sV0, 0, t0);
+        t0 = uniform(t0 + step);
+        if (t + 1 >= gr.steps) break;
+        wait_vmcnt<0>();
+        lds_barrier();
+        if (t + 2 < gr.steps) {
+          copy(sK0, sV0, t0 + step);
+          put_keys(t0 + step, 0);
+        }
+        blocks(sK1, sV1, 1, t0);
+        t0 = uniform(t0 + step);
       }
-      blocks(sK1, sV1, 1, t0);
-      t0 += step;
     }
   } else {
     PackStage<M> tk, tv;
