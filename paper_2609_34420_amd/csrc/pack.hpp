@@ -175,29 +175,42 @@ struct ScoreRef {
   bool fixed;
   float ref;
 };
-// From the workgroup's 256 entries (thread b: entry b, bias log2 e; 0 past the table).
-__device__ __forceinline__ ScoreRef score_ref(float entry, float cap2, float* lds) {
-  const bool mask = entry == -INFINITY;
-  float hi = mask ? -INFINITY : entry, lo = mask ? INFINITY : entry;
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) {
-    hi = fmaxf(hi, __shfl_xor(hi, o));
-    lo = fminf(lo, __shfl_xor(lo, o));
-  }
-  if ((threadIdx.x & 63) == 0) {
-    lds[2 * wave_id()] = hi;
-    lds[2 * wave_id() + 1] = lo;
-  }
-  __syncthreads();
+// The largest of a wave's values, wave-uniform (NaN passed over): within rows of 16
+// lanes by DPP, a hop of some cycles where one through LDS takes a hundred.
+__device__ __forceinline__ float wave_max(float x) {
+  const auto hop = [&](auto ctrl) {
+    const int y = __builtin_amdgcn_mov_dpp(__float_as_int(x), decltype(ctrl)::value, 0xf, 0xf, true);
+    x = fmaxf(x, __int_as_float(y));
+  };
+  hop(std::integral_constant<int, 0xB1>{});        // quad_perm 1 0 3 2
+  hop(std::integral_constant<int, 0x4E>{});        // quad_perm 2 3 0 1
+  hop(std::integral_constant<int, 0x141>{});       // row_half_mirror
+  hop(std::integral_constant<int, 0x140>{});       // row_mirror
+  const int v = __float_as_int(x);
+  return fmaxf(fmaxf(__int_as_float(__builtin_amdgcn_readlane(v, 0)), __int_as_float(__builtin_amdgcn_readlane(v, 16))),
+               fmaxf(__int_as_float(__builtin_amdgcn_readlane(v, 32)), __int_as_float(__builtin_amdgcn_readlane(v, 48))));
+}
+
+// Thread t's of the head's 256 entries (bias log2 e; 0 past the table) as bf16 capped
+// scores take them, and the reference. Every wave looks at all of them: no exchange.
+template <class M>
+__device__ __forceinline__ float capped_entry(const PackArgs& a, int h, ScoreRef& r) {
+  const int lane = threadIdx.x & 63, wave = wave_id();
+  const float cap2 = a.cap * kLog2e;
+  float own = 0.0f, hi = -INFINITY, lo = INFINITY;
 #pragma unroll
   for (int w = 0; w < kPackWaves; ++w) {
-    hi = fmaxf(hi, lds[2 * w]);
-    lo = fminf(lo, lds[2 * w + 1]);
+    const int b = w * 64 + lane;
+    const float e = M::entry(b < a.n_buckets ? a.table[(int64_t)h * a.n_buckets + b] : 0.0f, a, false);
+    hi = fmaxf(hi, e == -INFINITY ? hi : e);
+    lo = fminf(lo, e == -INFINITY ? lo : e);
+    own = wave == w ? e : own;
   }
-  ScoreRef r;
-  r.fixed = uniform(hi - lo + 2.0f * cap2 <= kSpan);   // (false for a NaN or infinite entry)
+  hi = wave_max(hi);
+  lo = -wave_max(-lo);
+  r.fixed = hi >= lo && hi - lo + 2.0f * cap2 <= kSpan;      // (not if all entries are masks)
   r.ref = r.fixed ? hi + cap2 - kBelow : 0.0f;
-  return r;
+  return own + (cap2 - r.ref);
 }
 
 // D: the tile's head dim (32 or 64); DS <= D: the tensors'.

@@ -107,11 +107,8 @@ __global__ __launch_bounds__(kPackThreads, M::D == 32 && M::BF16 ? 2 : (M::BF16 
         y = fmaxf(y, v[k].y);
       }
     }
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) {
-      x = fmaxf(x, __shfl_xor(x, o));
-      y = fmaxf(y, __shfl_xor(y, o));
-    }
+    x = wave_max(x);
+    y = wave_max(y);
     if (lane == 0) {
       red[0][wave] = x;
       red[1][wave] = y;

@@ -44,16 +44,11 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_dq_kernel(PackArgs a) {
   const int grp = wave >> lw, gw = wave & (W - 1);
   constexpr bool START = M::BF16 && !CAP;
   ScoreRef ref{false, 0.0f};
-  {
+  if constexpr (M::BF16 && CAP) {
+    sTab[threadIdx.x] = capped_entry<M>(a, h, ref);
+  } else {
     const int b = threadIdx.x;
-    float e = M::entry(b < a.n_buckets ? a.table[(int64_t)h * a.n_buckets + b] : 0.0f, a, START);
-    if constexpr (M::BF16 && CAP) {
-      const float cap2 = a.cap * kLog2e;
-      ref = score_ref(e, cap2, reinterpret_cast<float*>(sBuf0));
-      e += cap2 - ref.ref;
-      __syncthreads();
-    }
-    sTab[b] = e;
+    sTab[b] = M::entry(b < a.n_buckets ? a.table[(int64_t)h * a.n_buckets + b] : 0.0f, a, START);
   }
 
   const int off = gr.nk - gr.nq;
@@ -223,8 +218,7 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_dq_kernel(PackArgs a) {
   const float pm = ref.fixed ? exp2_fast(ref.ref + mlse) : 1.0f;
   dmax *= pm;
   dsum = (dsum + __shfl_xor(dsum, 32)) * pm;
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) dmax = fmaxf(dmax, __shfl_xor(dmax, o));
+  dmax = wave_max(dmax);
   if (gr.combine) {
     float* stat = reinterpret_cast<float*>(sBuf0 + NA * 16 * 64 * 4 * 2) + lane;
     pack_combine(
@@ -238,9 +232,7 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_dq_kernel(PackArgs a) {
                    [](int, float& wa, float& wo) { wa = wo = 1.0f; });
   }
   const bool mine = !gr.combine || grp == 0;             // the wave holds its rows' results
-  float cmax = mine ? fabsf(dsum) : 0.0f;
-#pragma unroll
-  for (int o = 16; o >= 1; o >>= 1) cmax = fmaxf(cmax, __shfl_xor(cmax, o));
+  const float cmax = wave_max(mine ? fabsf(dsum) : 0.0f);
   if (lane == 0) sMax[wave] = make_float2(dmax, cmax);
   if (mine && iok) {
     const float mul = a.scale * rp * pm * (CAP ? M::kSlope : 1.0f);

@@ -39,16 +39,11 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_fwd_kernel(PackArgs a) {
   const int grp = wave >> lw, gw = wave & (W - 1);
   constexpr bool START = M::BF16 && !CAP;              // the score accumulator starts from the bias
   ScoreRef fix{false, 0.0f};
-  {
+  if constexpr (M::BF16 && CAP) {
+    sTab[threadIdx.x] = capped_entry<M>(a, h, fix);
+  } else {
     const int b = threadIdx.x;
-    float e = M::entry(b < a.n_buckets ? a.table[(int64_t)h * a.n_buckets + b] : 0.0f, a, START);
-    if constexpr (M::BF16 && CAP) {
-      const float cap2 = a.cap * kLog2e;
-      fix = score_ref(e, cap2, reinterpret_cast<float*>(sBuf0));
-      e += cap2 - fix.ref;
-      __syncthreads();
-    }
-    sTab[b] = e;
+    sTab[b] = M::entry(b < a.n_buckets ? a.table[(int64_t)h * a.n_buckets + b] : 0.0f, a, START);
   }
 
   const int off = gr.nk - gr.nq;

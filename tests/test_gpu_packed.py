@@ -191,6 +191,26 @@ def test_masked_entries_and_empty_rows(dt, mask):
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("nb", [9, 256])
+def test_a_head_of_masks_alone(dt, nb):
+    """Every entry of one head's table a mask (256 buckets: of every byte)."""
+    n, H, d = [45, 130], 2, 16
+    a = make(n, n, H, d, nb, dt, seed=16)
+    a["spd"] %= min(nb, 255)
+    a["table"][1] = -np.inf
+    r = upload(a)
+    pack = gt.gt_attn_pack(n, H, device=DEV)
+    args = (r["q"], r["k"], r["v"], r["spd"], r["table"], pack)
+    for cap in (None, 6.0):
+        o, lse = gt.gt_attn_pack_fwd(*args, cap=cap, dropout=DROP)
+        grads = gt.gt_attn_pack_bwd(*args, o, lse, r["do"], cap=cap, dropout=DROP)
+        torch.cuda.synchronize()
+        assert bool((o[1] == 0).all()) and bool(torch.isneginf(lse[1]).all())
+        assert all(bool((x[1] == 0).all()) for x in grads)
+        assert all(bool(torch.isfinite(x[0].float()).all()) for x in (o, lse, *grads))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
 @pytest.mark.parametrize("cap,spread", [(200.0, 0.0), (30.0, 60.0), (30.0, 5.0), (1000.0, 0.0), (0.01, 0.0)])
 def test_ranges_of_capped_scores(dt, cap, spread):
     """Caps and biases whose scores span more than a fixed reference allows, and
