@@ -238,14 +238,15 @@ def measured_traffic(workload: str, kernel: str):
 
 # Device sources of the kernels the traffic record measured: every source
 # except the host-side C ABI and the kernels that the full-width workloads
-# never launch (the merge, and the short-sequence forward and backward).
+# never launch (the merge, the short-sequence forward and backward, and the
+# packed batches' sources, pack*).
 _HOST_OR_UNTIMED = {"api.hip", "merge.hip", "fwd_short.hip", "bwd_short.hip"}
 
 
 def kernel_sources_sha256() -> str:
     h = hashlib.sha256()
     for p in sorted((ROOT / "paper_2609_34420_amd" / "csrc").glob("*.[hc]*")):
-        if p.name in _HOST_OR_UNTIMED:
+        if p.name in _HOST_OR_UNTIMED or p.name.startswith("pack"):
             continue
         h.update(p.name.encode())
         h.update(p.read_bytes())
