@@ -365,7 +365,8 @@ gt_status_t gt_attn_bwd_ring_step(const void* q_shard, const void* o_shard,
  * Tensors of rows: element (h, row, c) at p + h head_stride + row row_stride + c,
  * strides in elements, so [H, rows, d] and [rows, H, d] layouts are taken as they
  * are. p 16-byte aligned, strides multiples of 16 bytes, row_stride from d to
- * 2^23; the rows of a written tensor do not overlap. Rows from the batch's total on are
+ * 2^23; the rows of a written tensor do not overlap. Heads that share a tensor have
+ * head_stride 0; its gradient is per head. Rows from the batch's total on are
  * neither read nor written. A captured graph reads the plan at each replay. */
 typedef struct {
   void* p;

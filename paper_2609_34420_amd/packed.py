@@ -12,8 +12,12 @@ header states the definitions).
 q, k, v [H, T, d] hold the graphs' rows one behind the other (T may be larger
 than their total: the rows behind it are left alone); any strides whose last is
 1 and whose others are multiples of 16 bytes, so a [T, H, d] tensor is passed as
-x.transpose(0, 1). spd holds the graphs' [n_q, n_k] uint8 distances one behind
+x.transpose(0, 1), and one that heads share as an expanded one (its gradient
+comes per head). spd holds the graphs' [n_q, n_k] uint8 distances one behind
 the other.
+
+Graphs of one size that take no cap, prefix or dropout run faster through
+gt_attn_fwd_batch and gt_attn_bwd_batch.
 """
 from __future__ import annotations
 
