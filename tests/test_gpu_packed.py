@@ -125,6 +125,28 @@ def test_new_rows_against_a_long_cache(dt, d, n):
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_generation_in_node_order(dt):
+    """Two graphs that grow node by node from the prefix they start with: each new
+    row against the keys so far, on the stored tensors as they lie, is the row of
+    the training forward (two results, each off by the tolerance)."""
+    n, H, d, pre = [60, 70], 2, 32, [20, 45]
+    r = upload(make(n, n, H, d, 22, dt, seed=17))
+    full = gt.gt_attn_pack(n, H, prefix=pre, device=DEV)
+    want, wl = gt.gt_attn_pack_fwd(r["q"], r["k"], r["v"], r["spd"], r["table"], full, cap=8.0)
+    # each graph's keys at the start of a slab of its own, 80 rows a graph
+    k, v = (torch.full((H, 160, d), float("nan"), device=DEV, dtype=r["q"].dtype) for _ in range(2))
+    for x, y in ((k, r["k"]), (v, r["v"])):
+        x[:, :60], x[:, 80:150] = y[:, :60], y[:, 60:]
+    for g, (n0, k0, q0, s0) in enumerate(((60, 0, 0, 0), (70, 80, 60, 3600))):
+        for t in range(pre[g] + 1, n0 + 1):
+            pack = gt.gt_attn_pack([1], H, n_k=[t], prefix=[pre[g]], spd_off=[s0 + (t - 1) * n0], spd_ld=[n0], device=DEV)
+            row = q0 + t - 1
+            o, lse = gt.gt_attn_pack_fwd(r["q"][:, row:row + 1], k[:, k0:], v[:, k0:], r["spd"], r["table"], pack, cap=8.0)
+            assert rel_l2(to_np(o[:, 0]), to_np(want[:, row])) <= 2 * TOL[dt]["o"], (g, t)
+            assert rel_l2(to_np(lse[:, 0]), to_np(wl[:, row])) <= 2 * TOL[dt]["f32"], (g, t)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
 @pytest.mark.parametrize("N", [300, 1000])
 @pytest.mark.parametrize("H", [1, 40])
 def test_split_and_unsplit_grids(dt, N, H):
@@ -136,6 +158,24 @@ def test_split_and_unsplit_grids(dt, N, H):
 @pytest.mark.parametrize("nb", [1, 2, 127, 128, 256])
 def test_bucket_counts(dt, nb):
     check(f"buckets {dt} nb={nb}", [150, 40], 2, 16, nb, dt, cap=8.0)
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_random_batches(seed):
+    """Seeded batches: sizes, heads, buckets, masks and options at random."""
+    g = np.random.default_rng(1000 + seed)
+    dt = ("bf16", "f32")[seed % 2]
+    top = int(g.choice([6, 40, 130, 400]))
+    n_k = [int(x) for x in g.integers(0, top + 1, int(g.integers(1, 24 if top < 400 else 5)))] + [top]
+    n_q = n_k if g.random() < 0.6 else [int(x) for x in g.integers(0, int(g.choice([3, top + 20])) + 1, len(n_k))]
+    if sum(n_q) == 0:
+        n_q = n_k
+    prefix = None if g.random() < 0.4 else [int(x) for x in g.integers(0, top + 2, len(n_k))]
+    drop = None if g.random() < 0.5 else gt.GTDropout(float(g.uniform(0.02, 0.6)), int(g.integers(1 << 62)), int(g.integers(1 << 32)))
+    # (a cap up to 30, uncapped scores up to some 8: the tolerances' sizes)
+    check(f"random {seed}", n_q, int(g.choice([1, 3, 8])), int(g.choice([8, 16, 32, 64])), int(g.choice([1, 20, 64, 130, 256])),
+          dt, n_k=n_k, prefix=prefix, cap=None if g.random() < 0.4 else float(g.uniform(1.0, 30.0)), drop=drop, seed=seed,
+          mask=0.0 if g.random() < 0.7 else 0.2)
 
 
 @pytest.mark.parametrize("drop", [None, gt.GTDropout(0.1, 21, 5)])
