@@ -379,6 +379,7 @@ typedef struct {
   int64_t spd_bytes;           /* bytes of distances that the batch reads from */
   int64_t plan_bytes;
   int32_t n_graphs, H;
+  int32_t backward;            /* 0: the plan serves gt_attn_pack_fwd alone */
   /* internal: the kernels' work lists inside the plan */
   int32_t jobs[3], merges, parts, slots;
   int64_t job_off[3], merge_off;
@@ -400,6 +401,8 @@ typedef struct {
  *   spd_off, spd_ld  [n_graphs] byte offset of a graph's [n_q, n_k] distances and
  *             their row stride (n_k .. 2^25 - 16), or NULL: the matrices lie dense, one
  *             behind the other
+ *   backward  0: without the backward's work lists, for evaluation and serving (they are
+ *             most of a plan where a few rows meet many keys)
  *   plan      NULL: only *info is filled; else host memory of plan_bytes bytes that
  *             receives the plan, which the caller copies to device memory (16-byte
  *             aligned) and passes to the calls as it is.
@@ -408,7 +411,7 @@ typedef struct {
  * host memory. All arrays are HOST arrays. */
 gt_status_t gt_attn_pack_plan(int32_t n_graphs, int32_t H, const int32_t* n_q, const int32_t* n_k,
                               const int32_t* prefix, const int64_t* spd_off, const int64_t* spd_ld,
-                              void* plan, size_t plan_bytes, gt_attn_pack_t* info);
+                              int32_t backward, void* plan, size_t plan_bytes, gt_attn_pack_t* info);
 
 /* Bytes of device workspace (256-byte aligned; contents ignored) of the two
  * calls; 0 for a forward that needs none. */

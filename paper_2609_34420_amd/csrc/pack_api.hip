@@ -151,6 +151,7 @@ gt_status_t gt_attn_pack_bwd(const gt_attn_pack_t* pack, const void* plan, const
   const gt_status_t st = gt::common(pack, plan, q, k, v, spd, table, n_buckets, o, lse, ld_lse, d, dtype, scale, cap,
                                     dropout, a);
   if (st != GT_OK) return st;
+  if (!pack->backward) return GT_ERR_INVALID;
   if (!gt::rows_ok(d_o, pack->total_q, d, dtype) || !gt::rows_ok(dq, pack->total_q, d, dtype) ||
       !gt::rows_ok(dk, pack->total_k, d, dtype) || !gt::rows_ok(dv, pack->total_k, d, dtype) || !dtable)
     return GT_ERR_INVALID;

@@ -223,7 +223,7 @@ int64_t place(size_t& at, const std::vector<T>& v, uint8_t* buf) {
 }
 
 gt_status_t make(int32_t G, int32_t H, const int32_t* n_q, const int32_t* n_k, const int32_t* prefix,
-                 const int64_t* spd_off, const int64_t* spd_ld, void* plan, size_t plan_bytes,
+                 const int64_t* spd_off, const int64_t* spd_ld, bool backward, void* plan, size_t plan_bytes,
                  gt_attn_pack_t* out) {
   std::vector<Graph> graphs;
   graphs.reserve(G);
@@ -253,10 +253,11 @@ gt_status_t make(int32_t G, int32_t H, const int32_t* n_q, const int32_t* n_k, c
   }
   info.n_graphs = G;
   info.H = H;
+  info.backward = backward;
   std::vector<PackWave> lists[3];
   std::vector<PackMerge> merges;
   const Stage stages[3] = {kForward, kDq, kDkdv};
-  for (int i = 0; i < 3; ++i) {
+  for (int i = 0; i < (backward ? 3 : 1); ++i) {
     const Plan p = best_plan(graphs, H, stages[i]);
     // (a launch counts its threads in 32 bits)
     if (((int64_t)p.jobs.size() + 8) * H * kPackWaves * 64 > std::numeric_limits<uint32_t>::max())
@@ -291,10 +292,10 @@ gt_status_t make(int32_t G, int32_t H, const int32_t* n_q, const int32_t* n_k, c
 
 extern "C" gt_status_t gt_attn_pack_plan(int32_t n_graphs, int32_t H, const int32_t* n_q, const int32_t* n_k,
                                          const int32_t* prefix, const int64_t* spd_off, const int64_t* spd_ld,
-                                         void* plan, size_t plan_bytes, gt_attn_pack_t* info) {
+                                         int32_t backward, void* plan, size_t plan_bytes, gt_attn_pack_t* info) {
   if (n_graphs < 1 || H < 1 || H > 65535 || !n_q || !n_k || !info) return GT_ERR_INVALID;
   try {
-    return gt::make(n_graphs, H, n_q, n_k, prefix, spd_off, spd_ld, plan, plan_bytes, info);
+    return gt::make(n_graphs, H, n_q, n_k, prefix, spd_off, spd_ld, backward != 0, plan, plan_bytes, info);
   } catch (...) {     // out of host memory
     return GT_ERR_WORKSPACE;
   }

@@ -139,7 +139,8 @@ def test_generation_in_node_order(dt):
         x[:, :60], x[:, 80:150] = y[:, :60], y[:, 60:]
     for g, (n0, k0, q0, s0) in enumerate(((60, 0, 0, 0), (70, 80, 60, 3600))):
         for t in range(pre[g] + 1, n0 + 1):
-            pack = gt.gt_attn_pack([1], H, n_k=[t], prefix=[pre[g]], spd_off=[s0 + (t - 1) * n0], spd_ld=[n0], device=DEV)
+            pack = gt.gt_attn_pack([1], H, n_k=[t], prefix=[pre[g]], spd_off=[s0 + (t - 1) * n0], spd_ld=[n0], device=DEV,
+                                   backward=False)
             row = q0 + t - 1
             o, lse = gt.gt_attn_pack_fwd(r["q"][:, row:row + 1], k[:, k0:], v[:, k0:], r["spd"], r["table"], pack, cap=8.0)
             assert rel_l2(to_np(o[:, 0]), to_np(want[:, row])) <= 2 * TOL[dt]["o"], (g, t)

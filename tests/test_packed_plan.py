@@ -120,6 +120,17 @@ def test_random_plans():
         check(n_q, n_k, prefix, rng.choice([1, 4, 16]))
 
 
+def test_plans_of_the_forward_alone():
+    """The forward's list is the same; the backward refuses the plan."""
+    n_q, n_k = [1, 3, 40, 0], [900, 5000, 40, 7]
+    a = gt.gt_attn_pack(n_q, 4, n_k=n_k, device="cpu")
+    b = gt.gt_attn_pack(n_q, 4, n_k=n_k, device="cpu", backward=False)
+    (x, y), (u, v) = lists(a), lists(b)
+    assert np.array_equal(x[0], u[0]) and np.array_equal(y, v) and len(u[1]) == len(u[2]) == 0
+    assert b._plan.numel() < a._plan.numel() and a.backward and not b.backward
+    assert (a.total_q, a.total_k, a.spd_bytes) == (b.total_q, b.total_k, b.spd_bytes)
+
+
 def test_plan_refusals():
     ok = dict(n_q=[3, 4], H=2, device="cpu")
     gt.gt_attn_pack(**ok)
@@ -141,16 +152,16 @@ def test_plan_c_abi():
     L, info = gt.lib(), gt.packed._Info()
     n = np.array([300, 20], np.int32)
     p = n.ctypes.data
-    assert L.gt_attn_pack_plan(2, 4, p, p, None, None, None, None, 0, ctypes.byref(info)) == 0
+    assert L.gt_attn_pack_plan(2, 4, p, p, None, None, None, 1, None, 0, ctypes.byref(info)) == 0
     need = info.plan_bytes
     assert need > 0 and info.total_q == 320 and info.spd_bytes == 300 * 300 + 20 * 20
     buf = np.zeros(need, np.uint8)
-    assert L.gt_attn_pack_plan(2, 4, p, p, None, None, None, buf.ctypes.data, need - 1, ctypes.byref(info)) == 3
+    assert L.gt_attn_pack_plan(2, 4, p, p, None, None, None, 1, buf.ctypes.data, need - 1, ctypes.byref(info)) == 3
     assert not buf.any()
-    assert L.gt_attn_pack_plan(2, 4, p, p, None, None, None, buf.ctypes.data, need, ctypes.byref(info)) == 0
+    assert L.gt_attn_pack_plan(2, 4, p, p, None, None, None, 1, buf.ctypes.data, need, ctypes.byref(info)) == 0
     for a in [(0, 4, p, p), (2, 0, p, p), (2, 4, None, p), (2, 4, p, None)]:
-        assert L.gt_attn_pack_plan(*a, None, None, None, None, 0, ctypes.byref(info)) == 1
-    assert L.gt_attn_pack_plan(2, 4, p, p, None, None, None, None, 0, None) == 1
+        assert L.gt_attn_pack_plan(*a, None, None, None, 1, None, 0, ctypes.byref(info)) == 1
+    assert L.gt_attn_pack_plan(2, 4, p, p, None, None, None, 1, None, 0, None) == 1
 
 
 # ---------------------------------------------------------------------------
@@ -161,14 +172,14 @@ FAKE, MIS = 0x10000, 0x10008
 
 def call(entry="fwd", **kw):
     a = dict(H=2, d=64, dtype=1, nb=8, scale=0.1, cap=0.0, p=None, ws=FAKE, wsb=1 << 30, plan=FAKE, spd=FAKE,
-             table=FAKE, lse=FAKE, ld=40, dtable=FAKE, offset_dev=None, info=True)
+             table=FAKE, lse=FAKE, ld=40, dtable=FAKE, offset_dev=None, info=True, backward=1)
     rows = {n: (FAKE, 40 * 64, 64) for n in ("q", "k", "v", "o", "d_o", "dq", "dk", "dv")}
     for k, x in kw.items():
         (rows if k in rows else a)[k] = x
     P = gt.packed
     n = np.array([30, 10], np.int32)
     info = P._Info()
-    assert gt.lib().gt_attn_pack_plan(2, a["H"], n.ctypes.data, n.ctypes.data, None, None, None, None, 0,
+    assert gt.lib().gt_attn_pack_plan(2, a["H"], n.ctypes.data, n.ctypes.data, None, None, None, a["backward"], None, 0,
                                       ctypes.byref(info)) == 0
     b = ctypes.byref
     r = {k: None if x is None else b(P._Rows(*x)) for k, x in rows.items()}
@@ -199,7 +210,7 @@ def test_call_refusals(entry, kw, code):
 
 @pytest.mark.parametrize("kw,code", [
     (dict(d_o=None), 1), (dict(dq=(None, 2560, 64)), 1), (dict(dk=(MIS, 2560, 64)), 1), (dict(dv=None), 1),
-    (dict(dtable=None), 1), (dict(ws=None), 3), (dict(wsb=0), 3), (dict(ws=FAKE + 16), 3)])
+    (dict(dtable=None), 1), (dict(backward=0), 1), (dict(ws=None), 3), (dict(wsb=0), 3), (dict(ws=FAKE + 16), 3)])
 def test_bwd_refusals(kw, code):
     assert call("bwd", **kw) == code
 
