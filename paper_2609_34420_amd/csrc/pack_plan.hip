@@ -172,7 +172,8 @@ std::vector<PackWave> waves(const std::vector<Graph>& graphs, const Plan& p) {
 // 16384 nodes, bf16 and fp32, head dims 16 to 64: within 5 % of the best of the three
 // nearly everywhere (7651 nodes, d = 64, bf16, backward: 888 / 947 / 1099 us with 1 / 2 /
 // 4; 1000 nodes 99 / 64 / 49; 16 graphs of 300: 59 / 71 / 80).
-double span(const Plan& p, int32_t H, Stage st, int s) {
+// full: the work bounds it, which a further split only adds to.
+double span(const Plan& p, int32_t H, Stage st, int s, bool& full) {
   const double per_block = s == 1 ? 1.0 : (s == 2 ? 1.05 : 1.2);
   double sum = 0.0, top = 0.0;
   for (const Job& j : p.jobs) {
@@ -183,22 +184,50 @@ double span(const Plan& p, int32_t H, Stage st, int s) {
   const double wgs = (double)p.jobs.size() * H;
   double slower = wgs <= 256.0 ? 1.0 : 1 / 0.7;
   if (st == kForward && wgs > 512.0) slower += 0.235 * (std::min(wgs / 256, 4.0) - 2.0);
-  return std::max(sum * H / (256 * 1.4), top * slower) + (p.parts ? 8.0 : 0.0);
+  const double work = sum * H / (256 * 1.4);
+  full = work >= top * slower;
+  return std::max(work, top * slower) + (p.parts ? 8.0 : 0.0);
 }
 
-Plan best_plan(const std::vector<Graph>& graphs, int32_t H, Stage st) {
-  Plan best = build(graphs, H, st, 1);
-  double cost = span(best, H, st, 1);
-  for (int s = 2; s <= 4; s *= 2) {
-    Plan p = build(graphs, H, st, s);
-    const double c = span(p, H, st, s);
-    if (c < 0.97 * cost) {
-      cost = c;
-      best = std::move(p);
-    }
+// The plans of the three stages. dQ's are the forward's where that has no parts, and
+// dK / dV's are dQ's in a batch without prefixes whose graphs have as many queries as
+// keys: each is built once, and lies in the plan once.
+class Plans {
+ public:
+  Plans(const std::vector<Graph>& graphs, int32_t H) : graphs_(graphs), H_(H) {
+    for (const Graph& g : graphs)
+      square_ = square_ && g.nq == g.nk && g.prefix == std::numeric_limits<int32_t>::max();
   }
-  return best;
-}
+  const Plan* best(Stage st) {
+    const Plan* best = nullptr;
+    double cost = 0.0;
+    bool full = false;
+    for (int i = 0; i < 3 && !full; ++i) {
+      const Plan& p = get(st, i);
+      const double c = span(p, H_, st, 1 << i, full);
+      if (!best || c < 0.97 * cost) {
+        cost = c;
+        best = &p;
+      }
+    }
+    return best;
+  }
+
+ private:
+  const Plan& get(Stage st, int i) {
+    if (st == kDkdv && square_) st = kDq;
+    if (st == kDq && made_[kForward][i] && plans_[kForward][i].parts == 0) st = kForward;
+    if (!made_[st][i]) {
+      plans_[st][i] = build(graphs_, H_, st, 1 << i);
+      made_[st][i] = true;
+    }
+    return plans_[st][i];
+  }
+  const std::vector<Graph>& graphs_;
+  const int32_t H_;
+  bool square_ = true, made_[3][3] = {};
+  Plan plans_[3][3];
+};
 
 // Workgroups per head of the key-stationary kernel, which take one job after the
 // other: the table, the histogram and its sums cost about as much as 16 blocks,
@@ -254,27 +283,31 @@ gt_status_t make(int32_t G, int32_t H, const int32_t* n_q, const int32_t* n_k, c
   info.n_graphs = G;
   info.H = H;
   info.backward = backward;
+  Plans plans(graphs, H);
+  const Plan* chosen[3] = {};
   std::vector<PackWave> lists[3];
-  std::vector<PackMerge> merges;
   const Stage stages[3] = {kForward, kDq, kDkdv};
   for (int i = 0; i < (backward ? 3 : 1); ++i) {
-    const Plan p = best_plan(graphs, H, stages[i]);
+    chosen[i] = plans.best(stages[i]);
+    const Plan& p = *chosen[i];
     // (a launch counts its threads in 32 bits)
     if (((int64_t)p.jobs.size() + 8) * H * kPackWaves * 64 > std::numeric_limits<uint32_t>::max())
       return GT_ERR_UNSUPPORTED;
-    lists[i] = waves(graphs, p);
+    if (std::find(chosen, chosen + i, &p) == chosen + i) lists[i] = waves(graphs, p);
     info.jobs[i] = (int32_t)p.jobs.size();
     if (i == kForward) {
-      merges = p.merges;
-      info.merges = (int32_t)merges.size();
+      info.merges = (int32_t)p.merges.size();
       info.parts = p.parts;
     }
     if (i == kDkdv) info.slots = slots(p, H);
   }
   auto lay_out = [&](uint8_t* buf) {
     size_t at = 0;
-    for (int i = 0; i < 3; ++i) info.job_off[i] = place(at, lists[i], buf);
-    info.merge_off = place(at, merges, buf);
+    for (int i = 0; i < 3; ++i) {
+      const int same = (int)(std::find(chosen, chosen + i, chosen[i]) - chosen);
+      info.job_off[i] = same < i ? info.job_off[same] : place(at, lists[i], buf);
+    }
+    info.merge_off = place(at, chosen[kForward]->merges, buf);
     info.plan_bytes = (int64_t)at;
   };
   lay_out(nullptr);

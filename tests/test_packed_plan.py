@@ -131,6 +131,13 @@ def test_plans_of_the_forward_alone():
     assert (a.total_q, a.total_k, a.spd_bytes) == (b.total_q, b.total_k, b.spd_bytes)
 
 
+def test_stages_share_a_list_where_they_can():
+    off = lambda **kw: list(gt.gt_attn_pack([700, 33, 90], 8, device="cpu", **kw)._info.job_off)
+    a, b = off(), off(prefix=[0, 5, 90])
+    assert a[0] == a[1] == a[2]
+    assert b[0] == b[1] < b[2]
+
+
 def test_plan_refusals():
     ok = dict(n_q=[3, 4], H=2, device="cpu")
     gt.gt_attn_pack(**ok)
