@@ -115,7 +115,7 @@ def gt_attn_pack(n_q, H: int, n_k=None, prefix=None, spd_off=None, spd_ld=None, 
     position (0: causal). spd_off, spd_ld: where a graph's distances lie in spd and
     their row stride, where they are not dense, one matrix behind the other.
     backward=False: a plan for the forward alone, sooner made where a few rows meet
-    many keys (the new nodes of 16 graphs of 1000 to 16000: 45 us for 520). Made
+    many keys (the new nodes of 16 graphs of 1000 to 16000: 45 us for 215). Made
     once per batch of sizes, it serves every layer's and step's calls; a captured
     graph reads it at each replay, so it has to live as long."""
     nq = _sizes(n_q, "n_q", None)
