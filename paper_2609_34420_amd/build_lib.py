@@ -22,7 +22,7 @@ BUILD_DIR = PKG / "_build"
 SOURCES = ["api.hip", "fwd.hip", "fwd_d64.hip", "fwd_d32.hip", "fwd_d16.hip", "fwd_d8.hip", "fwd_f32.hip",
            "bwd.hip", "bwd_dkdv.hip", "bwd_dq.hip", "bwd_short.hip", "bwd_f32.hip", "fwd_short.hip", "merge.hip",
            "pack_api.hip", "pack_plan.hip", "pack_fwd_bf16.hip", "pack_fwd_f32.hip", "pack_dq_bf16.hip",
-           "pack_dq_f32.hip", "pack_dkdv_bf16.hip", "pack_dkdv_f32.hip", "pack_sum.hip"]
+           "pack_dq_f32.hip", "pack_dkdv_bf16.hip", "pack_dkdv_f32.hip", "pack_short.hip", "pack_sum.hip"]
 ARCH = os.environ.get("GT_OFFLOAD_ARCH", "gfx950")
 
 

@@ -579,6 +579,27 @@ __device__ __forceinline__ void bias16(const float* tab, const uint32_t* w, floa
   for (int r = 0; r < 16; ++r) b[r] = tab[(w[r >> 2] >> (8 * (r & 3))) & 0xffu];
 }
 
+// Terms of the table gradient: floor(x + 0.5) for even r, -floor(0.5 - x), added by
+// subtraction, for odd r. The instruction rounds ties up, and ties are a quarter of all
+// values between 2^21 and 2^22 and half of those up to 2^23: with one direction for all
+// the bias grows with the pairs where the sum grows with their root (7651 nodes: the
+// table gradient off by 3e-5 against 1e-6). Rounding to even takes one
+// instruction more per pair (16384 nodes, d = 64: 2151 us, 2125 so).
+template <int ODD>
+__device__ __forceinline__ void add_term(unsigned long long* at, float x) {
+  int r;
+  if constexpr (ODD) {
+    asm("v_cvt_rpi_i32_f32 %0, -%1" : "=v"(r) : "v"(x));
+    __hip_atomic_fetch_sub(at, (unsigned long long)(long long)r, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+  } else {
+    asm("v_cvt_rpi_i32_f32 %0, %1" : "=v"(r) : "v"(x));
+    __hip_atomic_fetch_add(at, (unsigned long long)(long long)r, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+  }
+}
+
+// Buckets of the table gradient's histogram.
+inline int hist_buckets(int n_buckets) { return n_buckets < 32 ? 32 : (n_buckets < 64 ? 64 : (n_buckets < 128 ? 128 : 256)); }
+
 // Adds up the accumulators of groups that have the same rows (wave gw of group
 // ks into wave gw of group 0), pairwise and in a fixed order. buf: two waves'
 // accumulators. on_write(slot) and weights(slot, wa, wo) as in combine_groups.
@@ -628,6 +649,8 @@ hipError_t launch_pack_dq_bf16(const PackArgs& a, int d, bool cap, bool drop, hi
 hipError_t launch_pack_dq_f32(const PackArgs& a, int d, bool cap, bool drop, hipStream_t s);
 hipError_t launch_pack_dkdv_bf16(const PackArgs& a, int d, bool cap, bool drop, hipStream_t s);
 hipError_t launch_pack_dkdv_f32(const PackArgs& a, int d, bool cap, bool drop, hipStream_t s);
+// The whole backward of a batch of short graphs but for the sum of the table gradient.
+hipError_t launch_pack_short_bf16(const PackArgs& a, int d, bool cap, bool drop, hipStream_t s);
 hipError_t launch_pack_merge(const PackArgs& a, int d, bool bf16, hipStream_t s);
 hipError_t launch_pack_dtable(const PackArgs& a, hipStream_t s);
 

@@ -20,7 +20,8 @@ bool pack_ok(const gt_attn_pack_t* p) {
   if (!p || p->H < 1 || p->n_graphs < 1 || p->total_q < 0 || p->total_k < 0 || p->spd_bytes < 0) return false;
   for (int i = 0; i < 3; ++i)
     if (p->jobs[i] < 0 || p->job_off[i] < 0) return false;
-  return p->merges >= 0 && p->parts >= 0 && p->merge_off >= 0 && p->slots >= 0 && p->slots <= p->jobs[2];
+  return p->merges >= 0 && p->parts >= 0 && p->merge_off >= 0 && p->slots >= 0 && p->slots <= p->jobs[2] &&
+         p->short_jobs >= 0 && p->short_off >= 0 && p->short_slots >= 0 && p->short_slots <= p->short_jobs;
 }
 
 bool rows_ok(const gt_attn_rows_t* t, int64_t rows, int32_t d, gt_dtype_t dtype) {
@@ -96,7 +97,8 @@ BwdParts bwd_parts(const gt_attn_pack_t* p, int32_t n_buckets) {
   BwdParts b;
   b.dmax = pad256(H * (size_t)p->total_q * sizeof(float));
   b.dtab = b.dmax + pad256(H * (size_t)p->jobs[1] * sizeof(float2));
-  b.bytes = b.dtab + pad256(H * (size_t)p->slots * (size_t)n_buckets * sizeof(double));
+  const size_t slots = (size_t)(p->slots > p->short_slots ? p->slots : p->short_slots);
+  b.bytes = b.dtab + pad256(H * slots * (size_t)n_buckets * sizeof(double));
   return b;
 }
 
@@ -171,6 +173,14 @@ gt_status_t gt_attn_pack_bwd(const gt_attn_pack_t* pack, const void* plan, const
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const bool bf16 = dtype == GT_BF16, c = cap > 0.0f, drop = a.thr > -32768;
   hipError_t e = hipSuccess;
+  if (bf16 && pack->short_jobs > 0) {
+    a.jobs = reinterpret_cast<const gt::PackWave*>(static_cast<const uint8_t*>(plan) + pack->short_off);
+    a.njobs = pack->short_jobs;
+    a.slots = pack->short_slots;
+    e = gt::launch_pack_short_bf16(a, d, c, drop, s);
+    if (e == hipSuccess) e = gt::launch_pack_dtable(a, s);
+    return e == hipSuccess ? GT_OK : GT_ERR_LAUNCH;
+  }
   gt::stage(pack, plan, 1, a);
   if (a.njobs > 0) e = bf16 ? gt::launch_pack_dq_bf16(a, d, c, drop, s) : gt::launch_pack_dq_f32(a, d, c, drop, s);
   if (e != hipSuccess) return GT_ERR_LAUNCH;

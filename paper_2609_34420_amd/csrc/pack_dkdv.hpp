@@ -34,24 +34,6 @@ namespace gt {
 
 namespace {
 
-// Terms of the table gradient: floor(x + 0.5) for even r, -floor(0.5 - x), added by
-// subtraction, for odd r. The instruction rounds ties up, and ties are a quarter of all
-// values between 2^21 and 2^22 and half of those up to 2^23: with one direction for all
-// the bias grows with the pairs where the sum grows with their root (7651 nodes: the
-// table gradient off by 3e-5 against 1e-6). Rounding to even takes one
-// instruction more per pair (16384 nodes, d = 64: 2151 us, 2125 so).
-template <int ODD>
-__device__ __forceinline__ void add_term(unsigned long long* at, float x) {
-  int r;
-  if constexpr (ODD) {
-    asm("v_cvt_rpi_i32_f32 %0, -%1" : "=v"(r) : "v"(x));
-    __hip_atomic_fetch_sub(at, (unsigned long long)(long long)r, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-  } else {
-    asm("v_cvt_rpi_i32_f32 %0, %1" : "=v"(r) : "v"(x));
-    __hip_atomic_fetch_add(at, (unsigned long long)(long long)r, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-  }
-}
-
 // 32 x 32 bytes of a wave, 16 per lane row by row (lane l: row l / 2, from column
 // 16 (l & 1) on, or row l & 31, from column 16 (l >> 5) on), to the lane's column
 // (lane & 31), rows 16 g + 0 .. 15.
@@ -422,7 +404,7 @@ __global__ __launch_bounds__(kPackThreads, M::BF16 || M::D < 64 ? 2 : 1) void pa
 template <class M, bool CAP, bool DROP>
 void launch_pack_dkdv_nb(PackArgs a, hipStream_t s) {
   const dim3 grid(pack_grid(a.slots, a.H)), block(kPackThreads);
-  a.hist = a.n_buckets < 32 ? 32 : (a.n_buckets < 64 ? 64 : (a.n_buckets < 128 ? 128 : 256));
+  a.hist = hist_buckets(a.n_buckets);
   if (a.hist == 256)
     hipLaunchKernelGGL((pack_dkdv_kernel<M, CAP, DROP, true>), grid, block, 256 * 16 * 8, s, a);
   else

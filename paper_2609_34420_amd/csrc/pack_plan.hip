@@ -25,6 +25,8 @@ namespace {
 constexpr int64_t kMaxNodes = (1LL << 25) - 16;   // 32 rows of distances stay below 2^31 bytes
 constexpr int kSlots = 512;                       // workgroups that run at a time: two per compute unit
 
+constexpr int32_t kShortRows = 64;                // longest graph of the one-pass backward
+
 enum Stage { kForward, kDq, kDkdv };
 
 struct Graph {
@@ -242,6 +244,25 @@ int32_t slots(const Plan& p, int32_t H) {
   return (int32_t)std::min(n, std::max(by_work, full));
 }
 
+// The list of the backward of short graphs (at most two blocks of queries and of keys):
+// one group per graph, of the waves that its longer side takes. Empty if a graph is
+// longer.
+std::vector<PackWave> short_list(const std::vector<Graph>& graphs) {
+  std::vector<PackWave> out;
+  for (const Graph& g : graphs)
+    if (std::max(g.nq, g.nk) > kShortRows) return out;
+  for (int32_t lw = 1; lw >= 0; --lw) {
+    for (const Graph& g : graphs) {
+      const int32_t n = std::max(g.nq, g.nk);
+      if (n == 0 || (n > 32) != (lw == 1)) continue;
+      for (int32_t w = 0; w < 1 << lw; ++w)
+        out.push_back({g.q0, g.nq, g.k0, g.nk, w * 32, 0, g.nk, g.prefix, g.spd, g.ld, -1, lw, 0, 1, 0});
+    }
+    while (out.size() % kPackWaves) out.push_back({0, 0, 0, 0, 0, 0, 0, 0, 0, 0, -1, lw, 0, 1, 0});
+  }
+  return out;
+}
+
 template <typename T>
 int64_t place(size_t& at, const std::vector<T>& v, uint8_t* buf) {
   const size_t off = at;
@@ -301,6 +322,10 @@ gt_status_t make(int32_t G, int32_t H, const int32_t* n_q, const int32_t* n_k, c
     }
     if (i == kDkdv) info.slots = slots(p, H);
   }
+  std::vector<PackWave> shorts;
+  if (backward) shorts = short_list(graphs);
+  info.short_jobs = (int32_t)(shorts.size() / kPackWaves);
+  info.short_slots = std::min(info.short_jobs, (kSlots + H - 1) / H);
   auto lay_out = [&](uint8_t* buf) {
     size_t at = 0;
     for (int i = 0; i < 3; ++i) {
@@ -308,6 +333,7 @@ gt_status_t make(int32_t G, int32_t H, const int32_t* n_q, const int32_t* n_k, c
       info.job_off[i] = same < i ? info.job_off[same] : place(at, lists[i], buf);
     }
     info.merge_off = place(at, chosen[kForward]->merges, buf);
+    info.short_off = place(at, shorts, buf);
     info.plan_bytes = (int64_t)at;
   };
   lay_out(nullptr);
