@@ -600,6 +600,15 @@ __device__ __forceinline__ void add_term(unsigned long long* at, float x) {
 // Buckets of the table gradient's histogram.
 inline int hist_buckets(int n_buckets) { return n_buckets < 32 ? 32 : (n_buckets < 64 ? 64 : (n_buckets < 128 ? 128 : 256)); }
 
+// Workgroups of the one-pass backward of short graphs on a compute unit, by registers
+// and LDS: they are as many as fit, and take job after job.
+inline int hist_bytes(int n_buckets) { return hist_buckets(n_buckets) * (hist_buckets(n_buckets) == 256 ? 16 : 32) * 8; }
+inline int short_resident(int d, bool cap, bool drop, int n_buckets) {
+  const int lds = (d == 64 ? 66592 : 42016) + hist_bytes(n_buckets);
+  const int by_lds = 160 * 1024 / lds, by_registers = d == 64 || (cap && drop) ? 2 : 3;
+  return by_lds < by_registers ? by_lds : by_registers;
+}
+
 // Adds up the accumulators of groups that have the same rows (wave gw of group
 // ks into wave gw of group 0), pairwise and in a fixed order. buf: two waves'
 // accumulators. on_write(slot) and weights(slot, wa, wo) as in combine_groups.

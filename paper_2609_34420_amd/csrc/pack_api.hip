@@ -176,7 +176,8 @@ gt_status_t gt_attn_pack_bwd(const gt_attn_pack_t* pack, const void* plan, const
   if (bf16 && pack->short_jobs > 0) {
     a.jobs = reinterpret_cast<const gt::PackWave*>(static_cast<const uint8_t*>(plan) + pack->short_off);
     a.njobs = pack->short_jobs;
-    a.slots = pack->short_slots;
+    const int32_t fit = (gt::short_resident(d, c, drop, n_buckets) * 256 + a.H - 1) / a.H;
+    a.slots = fit < pack->short_slots ? fit : pack->short_slots;
     e = gt::launch_pack_short_bf16(a, d, c, drop, s);
     if (e == hipSuccess) e = gt::launch_pack_dtable(a, s);
     return e == hipSuccess ? GT_OK : GT_ERR_LAUNCH;

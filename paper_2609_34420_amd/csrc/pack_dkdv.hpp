@@ -406,9 +406,9 @@ void launch_pack_dkdv_nb(PackArgs a, hipStream_t s) {
   const dim3 grid(pack_grid(a.slots, a.H)), block(kPackThreads);
   a.hist = hist_buckets(a.n_buckets);
   if (a.hist == 256)
-    hipLaunchKernelGGL((pack_dkdv_kernel<M, CAP, DROP, true>), grid, block, 256 * 16 * 8, s, a);
+    hipLaunchKernelGGL((pack_dkdv_kernel<M, CAP, DROP, true>), grid, block, hist_bytes(a.n_buckets), s, a);
   else
-    hipLaunchKernelGGL((pack_dkdv_kernel<M, CAP, DROP, false>), grid, block, (unsigned)a.hist * 32 * 8, s, a);
+    hipLaunchKernelGGL((pack_dkdv_kernel<M, CAP, DROP, false>), grid, block, hist_bytes(a.n_buckets), s, a);
 }
 
 template <class M>

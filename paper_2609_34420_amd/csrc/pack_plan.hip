@@ -325,7 +325,7 @@ gt_status_t make(int32_t G, int32_t H, const int32_t* n_q, const int32_t* n_k, c
   std::vector<PackWave> shorts;
   if (backward) shorts = short_list(graphs);
   info.short_jobs = (int32_t)(shorts.size() / kPackWaves);
-  info.short_slots = std::min(info.short_jobs, (kSlots + H - 1) / H);
+  info.short_slots = std::min(info.short_jobs, (3 * 256 + H - 1) / H);
   auto lay_out = [&](uint8_t* buf) {
     size_t at = 0;
     for (int i = 0; i < 3; ++i) {

@@ -22,7 +22,7 @@ namespace gt {
 namespace {
 
 template <class M, bool CAP, bool DROP, bool WIDE>
-__global__ __launch_bounds__(kPackThreads, 2) void pack_short_kernel(PackArgs a) {
+__global__ __launch_bounds__(kPackThreads, M::D == 32 && !(CAP && DROP) ? 3 : 2) void pack_short_kernel(PackArgs a) {
   constexpr int NA = M::NA, D = M::D;
   constexpr int CPY = WIDE ? 16 : 32;
   constexpr int PT = 32 * 32;                               // elements of a tile of P or dU
@@ -86,14 +86,21 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_short_kernel(PackArgs a)
     wait_vmcnt<0>();
     lds_barrier();                                          // the tiles have landed
 
-    // P (in x), z dP (in dp) and the slope of both key blocks; the sum of P z dP
-    float x[2][16], dp[2][16], slope[2][16], zp[2][16];
+    // tile: queries as rows, the lane's row from key 16 g on
+    auto put = [&](uint16_t* tile, const float (&y)[16]) {
+      *reinterpret_cast<bf16x8*>(tile + col * 32 + swz_tile<32>(col, 2 * g) * 8) = cvt_bf16x8(y);
+      *reinterpret_cast<bf16x8*>(tile + col * 32 + swz_tile<32>(col, 2 * g + 1) * 8) = cvt_bf16x8(y + 8);
+    };
+    // P (in x), z dP (in dp) and the slope of both key blocks, z P into its tile; the
+    // sum of P z dP
+    float x[2][16], dp[2][16], slope[2][16];
     float dsum = 0.0f;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
       if (kb * 32 >= gr.nk || !active) {                    // (wave-uniform)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) x[kb][r] = dp[kb][r] = slope[kb][r] = zp[kb][r] = 0.0f;
+        for (int r = 0; r < 16; ++r) x[kb][r] = dp[kb][r] = 0.0f;
+        if (!active) put(sX[wave][kb], x[kb]);              // (keys without queries read it)
         continue;
       }
       align_spd5(w[kb], spd.sh);
@@ -120,18 +127,20 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_short_kernel(PackArgs a)
         rng.draw(rrow, rng.keys((uint32_t)(kb * 32 + 16 * g) / 8u), rw);
         rng.draw(rrow, rng.keys((uint32_t)(kb * 32 + 16 * g) / 8u + 1u), rw + 4);
       }
+      float zp[16];
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         x[kb][r] = M::expo(x[kb][r]);
         dp[kb][r] = t[r];
-        zp[kb][r] = x[kb][r];
+        zp[r] = x[kb][r];
         if constexpr (DROP) {
           const bool keep = kept(rw, r, a.thr);
           dp[kb][r] = keep ? dp[kb][r] : 0.0f;
-          zp[kb][r] = keep ? zp[kb][r] : 0.0f;
+          zp[r] = keep ? zp[r] : 0.0f;
         }
         dsum = fmaf(x[kb][r], dp[kb][r], dsum);
       }
+      put(sX[wave][kb], zp);
     }
     dsum += __shfl_xor(dsum, 32);                           // D (1 - p)
     float dmax = 0.0f;
@@ -203,11 +212,6 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_short_kernel(PackArgs a)
     for (int r = 0; r < 16; ++r) ok = ok && fabsf(acc[0][r]) < INFINITY;
     any_bad = any_bad || __any(iok && !ok);
 
-    // tile: queries as rows, the lane's row from key 16 g on
-    auto put = [&](uint16_t* tile, const float (&y)[16]) {
-      *reinterpret_cast<bf16x8*>(tile + col * 32 + swz_tile<32>(col, 2 * g) * 8) = cvt_bf16x8(y);
-      *reinterpret_cast<bf16x8*>(tile + col * 32 + swz_tile<32>(col, 2 * g + 1) * 8) = cvt_bf16x8(y + 8);
-    };
     auto product = [&](const uint16_t* rows, const uint16_t* tile, f32x16 (&y)[NA]) {
       M::cols(rows, lds_tr_operand(tile, p0, p1), lds_tr_operand(tile + 8 * 32, p0, p1), y);
     };
@@ -224,16 +228,12 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_short_kernel(PackArgs a)
 #pragma unroll
     for (int c = 0; c < NA; ++c) acc2[c] = zero_f32x16();
     if (lw == 0) {
-      put(sX[wave][0], zp[0]);
       put(sX[wave][1], x[0]);
       lds_barrier();
       product(sO[wave], sX[wave][0], acc);
       product(sQ[wave], sX[wave][1], acc2);
     } else {
       const int nqb = (gr.nq + 31) / 32;
-      put(sX[wave][0], zp[0]);
-      put(sX[wave][1], zp[1]);
-      lds_barrier();
       for (int qb = 0; qb < nqb; ++qb) product(sO[(grp << lw) + qb], sX[(grp << lw) + qb][gw], acc);
       lds_barrier();
       put(sX[wave][0], x[0]);
@@ -261,9 +261,9 @@ void launch_pack_short_nb(PackArgs a, hipStream_t s) {
   const dim3 grid(pack_grid(a.slots, a.H)), block(kPackThreads);
   a.hist = hist_buckets(a.n_buckets);
   if (a.hist == 256)
-    hipLaunchKernelGGL((pack_short_kernel<M, CAP, DROP, true>), grid, block, 256 * 16 * 8, s, a);
+    hipLaunchKernelGGL((pack_short_kernel<M, CAP, DROP, true>), grid, block, hist_bytes(a.n_buckets), s, a);
   else
-    hipLaunchKernelGGL((pack_short_kernel<M, CAP, DROP, false>), grid, block, (unsigned)a.hist * 32 * 8, s, a);
+    hipLaunchKernelGGL((pack_short_kernel<M, CAP, DROP, false>), grid, block, hist_bytes(a.n_buckets), s, a);
 }
 
 template <class M>
