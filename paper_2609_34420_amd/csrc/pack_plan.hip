@@ -25,7 +25,10 @@ namespace {
 constexpr int64_t kMaxNodes = (1LL << 25) - 16;   // 32 rows of distances stay below 2^31 bytes
 constexpr int kSlots = 512;                       // workgroups that run at a time: two per compute unit
 
-constexpr int32_t kShortRows = 64;                // longest graph of the one-pass backward
+// Longest graph of the one-pass backward: P and dP of 64 keys are 64 registers. It is the
+// faster one at every size measured (backward of 1024 graphs of 9 to 60 nodes, d = 8: 38
+// and 58 us; 300 of 40 to 64, d = 64, cap and dropout: 44 and 81; 8 of 10 to 40: the same).
+constexpr int32_t kShortRows = 64;
 
 enum Stage { kForward, kDq, kDkdv };
 

@@ -414,6 +414,98 @@ def test_offsets_past_32_bits():
     assert all(torch.equal(x, y) for x, y in zip((o, lse, dq, dk, dv, dt), want))
 
 
+# Batches whose graphs have at most 64 nodes take the one-pass backward in bf16.
+SHORT = [1, 31, 0, 32, 33, 64, 9, 50, 2, 60]
+
+
+@pytest.mark.parametrize("d", [8, 16, 32, 64])
+@pytest.mark.parametrize("cap,drop", [(None, None), (3.0, None), (None, DROP), (30.0, DROP)])
+@pytest.mark.parametrize("prefix", [None, "some"])
+def test_short_batch(d, cap, drop, prefix):
+    check(f"short d={d} cap={cap} drop={drop is not None} {prefix}", SHORT, 3, d, 20, "bf16", cap=cap, drop=drop,
+          prefix=prefix and [0, 40, 0, 5, 33, 0, 9, 20, 1, 0])
+
+
+@pytest.mark.parametrize("nb", [1, 31, 32, 64, 127, 128, 256])
+def test_short_batch_buckets(nb):
+    check(f"short nb={nb}", SHORT, 2, 16, nb, "bf16", cap=9.0)
+
+
+def test_short_batch_unlike_sides():
+    """Keys without queries, queries without keys, and one block against two."""
+    check("short sides", [0, 5, 20, 64, 40, 1, 33], 2, 32, 12, "bf16", n_k=[40, 0, 64, 20, 33, 64, 32], cap=5.0, drop=DROP)
+    check("short sides causal", [0, 5, 20, 64, 40, 1, 33], 2, 8, 12, "bf16", n_k=[40, 0, 64, 20, 33, 64, 32], prefix=[0] * 7)
+
+
+def test_short_batch_of_unlike_gradients():
+    """d_o of a graph up to 2^40 times another's, rising: the table gradient's scale
+    falls from job to job, of which a workgroup has several."""
+    n = [20 + g % 40 for g in range(800)]
+    H, d, nb = 8, 8, 4
+    a = make(n, n, H, d, nb, "bf16", seed=18)
+    at = 0
+    for g, w in enumerate(n):
+        a["do"][:, at:at + w] *= 2.0 ** (40 * g // len(n) - 20)
+        at += w
+    r = upload(a)
+    pack = gt.gt_attn_pack(n, H, device=DEV)
+    args = (r["q"], r["k"], r["v"], r["spd"], r["table"], pack)
+    o, lse = gt.gt_attn_pack_fwd(*args, cap=9.0)
+    got = gt.gt_attn_pack_bwd(*args, o, lse, r["do"], cap=9.0)
+    torch.cuda.synchronize()
+    assert pack._info.short_jobs > 2 * pack._info.short_slots
+    want = oracle.packed_backward(a["q"], a["k"], a["v"], a["spd"], a["table"], d ** -0.5, a["do"], n, n, cap=9.0)
+    at = 0
+    for w in n[:8]:                                        # the smallest gradients keep their own precision
+        for x, y in zip(got[:3], want[:3]):
+            assert rel_l2(to_np(x[:, at:at + w]), y[:, at:at + w]) <= 4 * TOL["bf16"]["grad"]
+        at += w
+    compare("unlike gradients", "bf16", [o, lse, *got], [to_np(o), to_np(lse), *want])
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_short_batch_nonfinite_and_repeated(bad):
+    n, H = [20, 40, 9, 60, 33, 64] * 30, 2
+    a = make(n, n, H, 32, 12, "bf16", seed=19)
+    r = upload(a)
+    pack = gt.gt_attn_pack(n, H, device=DEV)
+    args = (r["q"], r["k"], r["v"], r["spd"], r["table"], pack)
+    o, lse = gt.gt_attn_pack_fwd(*args, cap=9.0, dropout=DROP)
+    want = gt.gt_attn_pack_bwd(*args, o, lse, r["do"], cap=9.0, dropout=DROP)
+    for _ in range(3):
+        assert all(torch.equal(x, y) for x, y in zip(gt.gt_attn_pack_bwd(*args, o, lse, r["do"], cap=9.0, dropout=DROP), want))
+    for e in (-45, 40):
+        got = gt.gt_attn_pack_bwd(*args, o, lse, r["do"] * 2.0 ** e, cap=9.0, dropout=DROP)
+        assert all(torch.equal(x, y * 2.0 ** e) for x, y in zip(got, want)), e
+    do = r["do"].clone()
+    do[0, 25, 3] = bad                                     # head 0, the second graph, rows 20 .. 59
+    got = gt.gt_attn_pack_bwd(*args, o, lse, do, cap=9.0, dropout=DROP)
+    torch.cuda.synchronize()
+    for x, y in zip(got[:3], want[:3]):
+        assert torch.equal(x[:, :20], y[:, :20]) and torch.equal(x[:, 60:], y[:, 60:]) and torch.equal(x[1], y[1])
+    assert bool(torch.isnan(got[3][0]).all()) and torch.equal(got[3][1], want[3][1])
+
+
+def test_short_batch_captured():
+    n, H = [20, 40, 9, 60] * 40, 4
+    r = upload(make(n, n, H, 16, 22, "bf16", seed=20))
+    pack = gt.gt_attn_pack(n, H, device=DEV)
+    args = (r["q"], r["k"], r["v"], r["spd"], r["table"], pack)
+    step = lambda: (lambda f: (*f, *gt.gt_attn_pack_bwd(*args, *f, r["do"], dropout=DROP)))(
+        gt.gt_attn_pack_fwd(*args, dropout=DROP))
+    want = step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for k in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, want)), k
+        step()
+        torch.cuda.synchronize()
+
+
 def test_empty_batches():
     H, d = 2, 16
     t = torch.zeros(H, 3, device=DEV)
