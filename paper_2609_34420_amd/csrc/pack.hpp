@@ -603,9 +603,9 @@ inline int hist_buckets(int n_buckets) { return n_buckets < 32 ? 32 : (n_buckets
 // Workgroups of the one-pass backward of short graphs on a compute unit, by registers
 // and LDS: they are as many as fit, and take job after job.
 inline int hist_bytes(int n_buckets) { return hist_buckets(n_buckets) * (hist_buckets(n_buckets) == 256 ? 16 : 32) * 8; }
-inline int short_resident(int d, bool cap, bool drop, int n_buckets) {
-  const int lds = (d == 64 ? 66592 : 42016) + hist_bytes(n_buckets);
-  const int by_lds = 160 * 1024 / lds, by_registers = d == 64 || (cap && drop) ? 2 : 3;
+inline int short_resident(int d, int blocks, bool cap, bool drop, int n_buckets) {
+  const int lds = (d == 64 ? 66592 : (blocks == 4 ? 58400 : 42016)) + hist_bytes(n_buckets);
+  const int by_lds = 160 * 1024 / lds, by_registers = d == 64 || blocks == 4 || (cap && drop) ? 2 : 3;
   return by_lds < by_registers ? by_lds : by_registers;
 }
 
@@ -659,7 +659,8 @@ hipError_t launch_pack_dq_f32(const PackArgs& a, int d, bool cap, bool drop, hip
 hipError_t launch_pack_dkdv_bf16(const PackArgs& a, int d, bool cap, bool drop, hipStream_t s);
 hipError_t launch_pack_dkdv_f32(const PackArgs& a, int d, bool cap, bool drop, hipStream_t s);
 // The whole backward of a batch of short graphs but for the sum of the table gradient.
-hipError_t launch_pack_short_bf16(const PackArgs& a, int d, bool cap, bool drop, hipStream_t s);
+// blocks: of 32 rows that a graph has at most, 2, or 4 (d <= 32).
+hipError_t launch_pack_short_bf16(const PackArgs& a, int d, int blocks, bool cap, bool drop, hipStream_t s);
 hipError_t launch_pack_merge(const PackArgs& a, int d, bool bf16, hipStream_t s);
 hipError_t launch_pack_dtable(const PackArgs& a, hipStream_t s);
 

@@ -21,7 +21,8 @@ bool pack_ok(const gt_attn_pack_t* p) {
   for (int i = 0; i < 3; ++i)
     if (p->jobs[i] < 0 || p->job_off[i] < 0) return false;
   return p->merges >= 0 && p->parts >= 0 && p->merge_off >= 0 && p->slots >= 0 && p->slots <= p->jobs[2] &&
-         p->short_jobs >= 0 && p->short_off >= 0 && p->short_slots >= 0 && p->short_slots <= p->short_jobs;
+         p->short_jobs >= 0 && p->short_off >= 0 && p->short_slots >= 0 && p->short_slots <= p->short_jobs &&
+         (p->short_blocks == 2 || p->short_blocks == 4);
 }
 
 bool rows_ok(const gt_attn_rows_t* t, int64_t rows, int32_t d, gt_dtype_t dtype) {
@@ -83,6 +84,18 @@ gt_status_t common(const gt_attn_pack_t* pack, const void* plan, const gt_attn_r
 void stage(const gt_attn_pack_t* pack, const void* plan, int i, PackArgs& a) {
   a.jobs = reinterpret_cast<const PackWave*>(static_cast<const uint8_t*>(plan) + pack->job_off[i]);
   a.njobs = pack->jobs[i];
+}
+
+// The one-pass backward: faster than two passes wherever it was measured with up to two
+// blocks of keys (1024 graphs of 9 to 60 nodes, d = 8: 33 and 55 us; 300 of 40 to 64, d =
+// 64, cap and dropout: 43 and 80), and with up to four if two workgroups fit a compute
+// unit (2048 graphs of 85 to 92, d = 16, 22 buckets, cap: 310 and 401; 512 of 65 to 128,
+// d = 8, 64 buckets, of which one fits: 136 and 125) and not both a cap and dropout
+// take registers (2048 of 85 to 92: 466 and 470).
+bool short_applies(const gt_attn_pack_t* p, int32_t d, bool cap, bool drop, int32_t n_buckets) {
+  return p->short_jobs > 0 &&
+         (p->short_blocks == 2 ||
+          (d < 64 && !(cap && drop) && short_resident(d, p->short_blocks, cap, drop, n_buckets) == 2));
 }
 
 struct FwdParts { size_t lse, bytes; };
@@ -173,12 +186,12 @@ gt_status_t gt_attn_pack_bwd(const gt_attn_pack_t* pack, const void* plan, const
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const bool bf16 = dtype == GT_BF16, c = cap > 0.0f, drop = a.thr > -32768;
   hipError_t e = hipSuccess;
-  if (bf16 && pack->short_jobs > 0) {
+  if (bf16 && gt::short_applies(pack, d, c, drop, n_buckets)) {
     a.jobs = reinterpret_cast<const gt::PackWave*>(static_cast<const uint8_t*>(plan) + pack->short_off);
     a.njobs = pack->short_jobs;
-    const int32_t fit = (gt::short_resident(d, c, drop, n_buckets) * 256 + a.H - 1) / a.H;
+    const int32_t fit = (gt::short_resident(d, pack->short_blocks, c, drop, n_buckets) * 256 + a.H - 1) / a.H;
     a.slots = fit < pack->short_slots ? fit : pack->short_slots;
-    e = gt::launch_pack_short_bf16(a, d, c, drop, s);
+    e = gt::launch_pack_short_bf16(a, d, pack->short_blocks, c, drop, s);
     if (e == hipSuccess) e = gt::launch_pack_dtable(a, s);
     return e == hipSuccess ? GT_OK : GT_ERR_LAUNCH;
   }

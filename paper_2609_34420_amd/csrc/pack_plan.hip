@@ -25,10 +25,8 @@ namespace {
 constexpr int64_t kMaxNodes = (1LL << 25) - 16;   // 32 rows of distances stay below 2^31 bytes
 constexpr int kSlots = 512;                       // workgroups that run at a time: two per compute unit
 
-// Longest graph of the one-pass backward: P and dP of 64 keys are 64 registers. It is the
-// faster one at every size measured (backward of 1024 graphs of 9 to 60 nodes, d = 8: 38
-// and 58 us; 300 of 40 to 64, d = 64, cap and dropout: 44 and 81; 8 of 10 to 40: the same).
-constexpr int32_t kShortRows = 64;
+// Longest graph of the one-pass backward: P and dP of 128 keys are 128 registers.
+constexpr int32_t kShortRows = 128;
 
 enum Stage { kForward, kDq, kDkdv };
 
@@ -247,17 +245,19 @@ int32_t slots(const Plan& p, int32_t H) {
   return (int32_t)std::min(n, std::max(by_work, full));
 }
 
-// The list of the backward of short graphs (at most two blocks of queries and of keys):
+// The list of the one-pass backward, and the blocks of 32 rows that a graph has at most:
 // one group per graph, of the waves that its longer side takes. Empty if a graph is
 // longer.
-std::vector<PackWave> short_list(const std::vector<Graph>& graphs) {
+std::vector<PackWave> short_list(const std::vector<Graph>& graphs, int32_t& blocks) {
   std::vector<PackWave> out;
-  for (const Graph& g : graphs)
-    if (std::max(g.nq, g.nk) > kShortRows) return out;
-  for (int32_t lw = 1; lw >= 0; --lw) {
+  int32_t top = 0;
+  for (const Graph& g : graphs) top = std::max(top, std::max(g.nq, g.nk));
+  blocks = top <= 64 ? 2 : 4;
+  if (top > kShortRows) return out;
+  for (int32_t lw = 2; lw >= 0; --lw) {
     for (const Graph& g : graphs) {
       const int32_t n = std::max(g.nq, g.nk);
-      if (n == 0 || (n > 32) != (lw == 1)) continue;
+      if (n == 0 || (n > 64 ? 2 : (n > 32 ? 1 : 0)) != lw) continue;
       for (int32_t w = 0; w < 1 << lw; ++w)
         out.push_back({g.q0, g.nq, g.k0, g.nk, w * 32, 0, g.nk, g.prefix, g.spd, g.ld, -1, lw, 0, 1, 0});
     }
@@ -326,7 +326,8 @@ gt_status_t make(int32_t G, int32_t H, const int32_t* n_q, const int32_t* n_k, c
     if (i == kDkdv) info.slots = slots(p, H);
   }
   std::vector<PackWave> shorts;
-  if (backward) shorts = short_list(graphs);
+  info.short_blocks = 2;
+  if (backward) shorts = short_list(graphs, info.short_blocks);
   info.short_jobs = (int32_t)(shorts.size() / kPackWaves);
   info.short_slots = std::min(info.short_jobs, (3 * 256 + H - 1) / H);
   auto lay_out = [&](uint8_t* buf) {

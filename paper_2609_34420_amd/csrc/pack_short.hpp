@@ -1,7 +1,8 @@
-// Backward of packed batches whose graphs have at most 64 queries and keys, bf16
-// (instantiated in pack_short.hip): dQ, dK, dV and the table gradient in one pass.
+// Backward of packed batches whose graphs have at most 64 (NK = 2) or 128 (NK = 4)
+// queries and keys, bf16 (instantiated in pack_short.hip): dQ, dK, dV and the table
+// gradient in one pass.
 //
-// A wave has 32 queries and all the keys of its graph, one or two blocks of 32, so a
+// A wave has 32 queries and all the keys of its graph, up to NK blocks of 32, so a
 // row's P and dP stay in registers until its sum D = sum_j P z dP is whole: D is
 // exact, O is not needed, and each score is formed once.
 //   S^T = K Q^T, dP^T = V dO^T, dS = P (z dP / (1 - p) - D), dU = dS (1 - tanh^2),
@@ -16,14 +17,17 @@
 // falls, and the sums are shifted when it does. The workgroups take job after job and
 // give one sum each.
 //
-// P and dU are rounded to bf16 as the operands of their products (2^-8 of a term).
+// P and dU are rounded to bf16 as the operands of their products (2^-8 of a term); the
+// cap's slope waits in fp16, two to a register (2^-11 of dU; 1 - tanh^2 comes out of
+// fp32 with an error of 2^-22 at least, fp16's step at the low end).
 //
 // Bound: set-up and latency of jobs of one or two blocks, and issue (vector units busy
 // 68 %, with a third or half of the lanes past their graph): 1024 graphs of 9 to 60
-// nodes, H = 8, d = 8, cap: 32 us, where dQ and dK / dV took 25 and 31; 4000 of 50
-// to 64: 150; 2048 of 16 to 40 at d = 64, 256 buckets: 163 for 206. Longer graphs
-// keep the two passes: their P and dP do not fit a wave's registers, and D from O is
-// not exact enough for the table gradient. A job's record read a job ahead gained 1 %.
+// nodes, H = 8, d = 8, cap: 30 us, where dQ and dK / dV took 25 and 31; 4000 of 50
+// to 64: 144; 2048 of 16 to 40 at d = 64, 256 buckets: 163 for 206; 2048 of 85 to 92 at
+// d = 16, cap: 300 for 390. Longer graphs keep the two passes: their P and dP do not fit
+// a wave's registers, and D from O is not exact enough for the table gradient. A job's
+// record read a job ahead gained 1 %.
 #pragma once
 #include "pack.hpp"
 
@@ -31,15 +35,18 @@ namespace gt {
 
 namespace {
 
-template <class M, bool CAP, bool DROP, bool WIDE>
-__global__ __launch_bounds__(kPackThreads, M::D == 32 && !(CAP && DROP) ? 3 : 2) void pack_short_kernel(PackArgs a) {
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+// NK: blocks of 32 keys that a graph has at most (2 or 4).
+template <class M, int NK, bool CAP, bool DROP, bool WIDE>
+__global__ __launch_bounds__(kPackThreads, NK == 2 && M::D == 32 && !(CAP && DROP) ? 3 : 2) void pack_short_kernel(PackArgs a) {
   constexpr int NA = M::NA, D = M::D;
   constexpr int CPY = WIDE ? 16 : 32;
   constexpr int PT = 32 * 32;                               // elements of a tile of P or dU
   extern __shared__ unsigned long long hist[];              // a.hist buckets of CPY copies
   __shared__ alignas(4096) float sTab[256];
   __shared__ alignas(128) uint16_t sK[kPackWaves][M::TILE], sQ[kPackWaves][M::TILE], sO[kPackWaves][M::TILE];
-  __shared__ alignas(128) uint16_t sX[kPackWaves][2][PT];
+  __shared__ alignas(128) uint16_t sX[kPackWaves][NK][PT];
   __shared__ float red[kPackWaves];
   __shared__ int bad[kPackWaves];
 
@@ -72,6 +79,10 @@ __global__ __launch_bounds__(kPackThreads, M::D == 32 && !(CAP && DROP) ? 3 : 2)
     const int vis = ic + gr.nk - gr.nq + 1 > gr.prefix ? ic + gr.nk - gr.nq + 1 : gr.prefix;
     const int lim = iok ? (vis < gr.nk ? vis : gr.nk) : 0;    // visible keys of the lane's query
 
+    const int il = iw + 31 < gr.nq ? iw + 31 : gr.nq - 1;
+    const int vl = il + gr.nk - gr.nq + 1 > gr.prefix ? il + gr.nk - gr.nq + 1 : gr.prefix;
+    const int lim1 = active ? (vl < gr.nk ? vl : gr.nk) : 0;  // of the wave's queries
+
     lds_barrier();                                          // the last job's tiles are read, the table is written
     cq.load(rows_at<const uint16_t>(a.q, h, gr.q0), a.q.rs, iw, gr.nq, sQ[wave]);
     co.load(rows_at<const uint16_t>(a.d_o, h, gr.q0), a.d_o.rs, iw, gr.nq, sO[wave]);
@@ -82,11 +93,14 @@ __global__ __launch_bounds__(kPackThreads, M::D == 32 && !(CAP && DROP) ? 3 : 2)
     const uint16_t* vh = rows_at<const uint16_t>(a.v, h, gr.k0);
     const PackSpdRow spd(a.spd + gr.spd + (int64_t)(active ? iw : 0) * gr.ld, gr.ld, active ? gr.nq - iw : 1,
                          active ? gr.nk : 0);
-    uint32_t w[2][5];
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
+    uint32_t w[NK][5];
+    auto load_v = [&](int kb) {
       const int j = kb * 32 + perm32(col);
-      M::load_operand(vh + (j < gr.nk ? j : 0) * a.v.rs, j < gr.nk, 1.0f, v[kb]);
+      M::load_operand(vh + (j < gr.nk ? j : 0) * a.v.rs, j < gr.nk, 1.0f, v[kb & 1]);
+    };
+#pragma unroll
+    for (int kb = 0; kb < NK; ++kb) {
+      if (kb < 2) load_v(kb);
       spd.fetch(kb * 32, w[kb]);
     }
     const float lse = iok ? a.lse[h * a.ld_lse + gr.q0 + ic] : -INFINITY;
@@ -103,14 +117,15 @@ __global__ __launch_bounds__(kPackThreads, M::D == 32 && !(CAP && DROP) ? 3 : 2)
     };
     // P (in x), z dP (in dp) and the slope of both key blocks, z P into its tile; the
     // sum of P z dP
-    float x[2][16], dp[2][16], slope[2][16];
+    float x[NK][16], dp[NK][16];
+    f16x2 slope[NK][8];
     float dsum = 0.0f;
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      if (kb * 32 >= gr.nk || !active) {                    // (wave-uniform)
+    for (int kb = 0; kb < NK; ++kb) {
+      if (kb * 32 >= lim1) {                                // no visible key (wave-uniform)
 #pragma unroll
         for (int r = 0; r < 16; ++r) x[kb][r] = dp[kb][r] = 0.0f;
-        if (!active) put(sX[wave][kb], x[kb]);              // (keys without queries read it)
+        put(sX[wave][kb], x[kb]);
         continue;
       }
       align_spd5(w[kb], spd.sh);
@@ -122,12 +137,16 @@ __global__ __launch_bounds__(kPackThreads, M::D == 32 && !(CAP && DROP) ? 3 : 2)
       }
       M::rows(sK[(grp << lw) + kb], q, s);
 #pragma unroll
-      for (int kc = 0; kc < (M::DS + 15) / 16; ++kc) t = mfma32(v[kb].f[kc], d_o.f[kc], t);
+      for (int kc = 0; kc < (M::DS + 15) / 16; ++kc) t = mfma32(v[kb & 1].f[kc], d_o.f[kc], t);
+      if (kb + 2 < NK) load_v(kb + 2);
       if constexpr (START) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) x[kb][r] = fmaf(s[r], sc.mul, mlse);
       } else {
-        M::template scores<CAP, true>(s, x[kb], slope[kb], sc);
+        float sl[16];
+        M::template scores<CAP, true>(s, x[kb], sl, sc);
+#pragma unroll
+        for (int r = 0; r < 16; r += 2) slope[kb][r / 2] = f16x2{(_Float16)sl[r], (_Float16)sl[r + 1]};
 #pragma unroll
         for (int r = 0; r < 16; ++r) x[kb][r] += mlse;
       }
@@ -155,7 +174,7 @@ __global__ __launch_bounds__(kPackThreads, M::D == 32 && !(CAP && DROP) ? 3 : 2)
     dsum += __shfl_xor(dsum, 32);                           // D (1 - p)
     float dmax = 0.0f;
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+    for (int kb = 0; kb < NK; ++kb)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         x[kb][r] *= dp[kb][r] - dsum;                       // dS (1 - p)
@@ -183,8 +202,8 @@ __global__ __launch_bounds__(kPackThreads, M::D == 32 && !(CAP && DROP) ? 3 : 2)
 #pragma unroll
     for (int c = 0; c < NA; ++c) acc[c] = zero_f32x16();
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      if (kb * 32 >= gr.nk || !active) continue;
+    for (int kb = 0; kb < NK; ++kb) {
+      if (kb * 32 >= lim1) continue;
       uint32_t (&b)[5] = w[kb];
       if constexpr (!WIDE) {
         // bytes past the layout go to its last bucket
@@ -206,7 +225,7 @@ __global__ __launch_bounds__(kPackThreads, M::D == 32 && !(CAP && DROP) ? 3 : 2)
           add_term<0>(e, x[kb][r] * sF);
         else
           add_term<1>(e, x[kb][r] * sF);
-        if constexpr (CAP) x[kb][r] *= slope[kb][r];
+        if constexpr (CAP) x[kb][r] *= (float)slope[kb][r / 2][r & 1];
       }
       M::cols(sK[(grp << lw) + kb], x[kb], acc);
     }
@@ -246,8 +265,8 @@ __global__ __launch_bounds__(kPackThreads, M::D == 32 && !(CAP && DROP) ? 3 : 2)
       const int nqb = (gr.nq + 31) / 32;
       for (int qb = 0; qb < nqb; ++qb) product(sO[(grp << lw) + qb], sX[(grp << lw) + qb][gw], acc);
       lds_barrier();
-      put(sX[wave][0], x[0]);
-      put(sX[wave][1], x[1]);
+#pragma unroll
+      for (int kb = 0; kb < NK; ++kb) put(sX[wave][kb], x[kb]);
       lds_barrier();
       for (int qb = 0; qb < nqb; ++qb) product(sQ[(grp << lw) + qb], sX[(grp << lw) + qb][gw], acc2);
     }
@@ -266,26 +285,29 @@ __global__ __launch_bounds__(kPackThreads, M::D == 32 && !(CAP && DROP) ? 3 : 2)
   }
 }
 
-template <class M, bool CAP, bool DROP>
+template <class M, int NK, bool CAP, bool DROP>
 void launch_pack_short_nb(PackArgs a, hipStream_t s) {
   const dim3 grid(pack_grid(a.slots, a.H)), block(kPackThreads);
   a.hist = hist_buckets(a.n_buckets);
   if (a.hist == 256)
-    hipLaunchKernelGGL((pack_short_kernel<M, CAP, DROP, true>), grid, block, hist_bytes(a.n_buckets), s, a);
+    hipLaunchKernelGGL((pack_short_kernel<M, NK, CAP, DROP, true>), grid, block, hist_bytes(a.n_buckets), s, a);
   else
-    hipLaunchKernelGGL((pack_short_kernel<M, CAP, DROP, false>), grid, block, hist_bytes(a.n_buckets), s, a);
+    hipLaunchKernelGGL((pack_short_kernel<M, NK, CAP, DROP, false>), grid, block, hist_bytes(a.n_buckets), s, a);
 }
 
-template <class M>
+template <class M, int NK>
 hipError_t launch_pack_short(const PackArgs& a, bool cap, bool drop, hipStream_t s) {
-  if (cap && drop)
-    launch_pack_short_nb<M, true, true>(a, s);
-  else if (cap)
-    launch_pack_short_nb<M, true, false>(a, s);
+  if (cap && drop) {
+    if constexpr (NK == 2)
+      launch_pack_short_nb<M, NK, true, true>(a, s);
+    else
+      return hipErrorInvalidValue;                          // (such calls take two passes)
+  } else if (cap)
+    launch_pack_short_nb<M, NK, true, false>(a, s);
   else if (drop)
-    launch_pack_short_nb<M, false, true>(a, s);
+    launch_pack_short_nb<M, NK, false, true>(a, s);
   else
-    launch_pack_short_nb<M, false, false>(a, s);
+    launch_pack_short_nb<M, NK, false, false>(a, s);
   return hipGetLastError();
 }
 

@@ -426,6 +426,17 @@ def test_short_batch(d, cap, drop, prefix):
           prefix=prefix and [0, 40, 0, 5, 33, 0, 9, 20, 1, 0])
 
 
+@pytest.mark.parametrize("d", [8, 16, 32, 64])
+@pytest.mark.parametrize("cap,drop", [(None, None), (3.0, None), (0.05, None), (None, DROP), (30.0, DROP)])
+@pytest.mark.parametrize("prefix", [None, "some"])
+def test_short_batch_of_four_blocks(d, cap, drop, prefix):
+    """Up to 128 nodes, the second list of sizes with unlike sides."""
+    n = [128, 65, 1, 33, 64, 0, 97, 96, 100, 31]
+    kw = dict(cap=cap, drop=drop, prefix=prefix and [0, 40, 0, 5, 33, 0, 9, 120, 1, 0])
+    check(f"four blocks d={d} cap={cap} drop={drop is not None} {prefix}", n, 3, d, 20, "bf16", **kw)
+    check("unlike sides", n, 1, d, 20, "bf16", n_k=[3, 128, 70, 0, 100, 40, 97, 128, 1, 31], **kw)
+
+
 @pytest.mark.parametrize("nb", [1, 31, 32, 64, 127, 128, 256])
 def test_short_batch_buckets(nb):
     check(f"short nb={nb}", SHORT, 2, 16, nb, "bf16", cap=9.0)

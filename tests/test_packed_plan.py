@@ -144,9 +144,9 @@ def test_short_list_has_every_graph_once():
         i = p._info
         return p, p._plan.numpy()[i.short_off:][:4 * i.short_jobs * WAVE.itemsize].view(WAVE).reshape(-1, 4)
 
-    n_q = [1, 31, 0, 32, 33, 64, 9, 50, 2, 60, 5, 0]
-    n_k = [1, 31, 7, 0, 64, 20, 9, 50, 40, 60, 5, 0]
-    p, jobs = short(n_q, n_k=n_k, prefix=list(range(12)))
+    n_q = [1, 31, 0, 32, 33, 64, 9, 50, 2, 60, 5, 0, 128, 65, 3]
+    n_k = [1, 31, 7, 0, 64, 20, 9, 50, 40, 60, 5, 0, 7, 128, 96]
+    p, jobs = short(n_q, n_k=n_k, prefix=list(range(15)))
     assert 0 < p._info.short_slots <= p._info.short_jobs
     seen = []
     for job in jobs:
@@ -157,14 +157,15 @@ def test_short_list_has_every_graph_once():
             if max(w[0]["nq"], w[0]["nk"]) == 0:
                 continue
             assert list(w["row"]) == [32 * k for k in range(1 << lw)]
-            assert max(w[0]["nq"], w[0]["nk"]) <= 32 << lw and max(w[0]["nq"], w[0]["nk"]) > 32 * lw
+            assert max(w[0]["nq"], w[0]["nk"]) <= 32 << lw and max(w[0]["nq"], w[0]["nk"]) > [0, 32, 64][lw]
             assert all((w[f] == w[0][f]).all() for f in ("q0", "nq", "k0", "nk", "prefix", "spd", "ld"))
             seen.append(tuple(int(w[0][f]) for f in ("q0", "nq", "k0", "nk", "prefix")))
     a = np.concatenate([[0], np.cumsum(n_q)])
     b = np.concatenate([[0], np.cumsum(n_k)])
-    assert sorted(seen) == sorted((int(a[g]), n_q[g], int(b[g]), n_k[g], g) for g in range(12) if n_q[g] or n_k[g])
-    assert short([64, 3])[0]._info.short_jobs == 2 and short([65, 3])[0]._info.short_jobs == 0
-    assert short([5, 5], n_k=[5, 65])[0]._info.short_jobs == 0 and short([5], backward=False)[0]._info.short_jobs == 0
+    assert sorted(seen) == sorted((int(a[g]), n_q[g], int(b[g]), n_k[g], g) for g in range(15) if n_q[g] or n_k[g])
+    blocks = lambda *a, **kw: (lambda i: (i.short_jobs, i.short_blocks))(short(*a, **kw)[0]._info)
+    assert blocks([64, 3]) == (2, 2) and blocks([65, 3]) == (2, 4) and short([129, 3])[0]._info.short_jobs == 0
+    assert short([5, 5], n_k=[5, 129])[0]._info.short_jobs == 0 and short([5], backward=False)[0]._info.short_jobs == 0
 
 
 def test_plan_refusals():
