@@ -32,8 +32,9 @@ namespace gt {
 
 namespace {
 
-template <class M, bool CAP, bool DROP>
-__global__ __launch_bounds__(kPackThreads, 2) void pack_dq_kernel(PackArgs a) {
+// WPS: waves per SIMD that the registers are shared by.
+template <class M, bool CAP, bool DROP, int WPS>
+__global__ __launch_bounds__(kPackThreads, WPS) void pack_dq_kernel(PackArgs a) {
   using T = typename M::T;
   constexpr int NA = M::NA;
   constexpr int NB = M::BF16 ? 2 : 1;                            // staged tiles
@@ -268,18 +269,29 @@ __global__ __launch_bounds__(kPackThreads, 2) void pack_dq_kernel(PackArgs a) {
   }
 }
 
-template <class M>
-hipError_t launch_pack_dq(const PackArgs& a, bool cap, bool drop, hipStream_t s) {
+template <class M, int WPS>
+hipError_t launch_pack_dq_wps(const PackArgs& a, bool cap, bool drop, hipStream_t s) {
   const dim3 grid(pack_grid(a.njobs, a.H)), block(kPackThreads);
   if (cap && drop)
-    hipLaunchKernelGGL((pack_dq_kernel<M, true, true>), grid, block, 0, s, a);
+    hipLaunchKernelGGL((pack_dq_kernel<M, true, true, WPS>), grid, block, 0, s, a);
   else if (cap)
-    hipLaunchKernelGGL((pack_dq_kernel<M, true, false>), grid, block, 0, s, a);
+    hipLaunchKernelGGL((pack_dq_kernel<M, true, false, WPS>), grid, block, 0, s, a);
   else if (drop)
-    hipLaunchKernelGGL((pack_dq_kernel<M, false, true>), grid, block, 0, s, a);
+    hipLaunchKernelGGL((pack_dq_kernel<M, false, true, WPS>), grid, block, 0, s, a);
   else
-    hipLaunchKernelGGL((pack_dq_kernel<M, false, false>), grid, block, 0, s, a);
+    hipLaunchKernelGGL((pack_dq_kernel<M, false, false, WPS>), grid, block, 0, s, a);
   return hipGetLastError();
+}
+
+// At two waves per SIMD the fp32 kernel at d = 64 spills 19 to 31 registers. With a
+// workgroup per compute unit or less there is nothing to share them with (2000 nodes,
+// H = 4: 137 us, 90 with all registers); with more the second wave is worth it (8 graphs
+// of 1000: 163 and 168).
+template <class M>
+hipError_t launch_pack_dq(const PackArgs& a, bool cap, bool drop, hipStream_t s) {
+  if constexpr (!M::BF16 && M::D == 64)
+    if ((int64_t)a.njobs * a.H <= 256) return launch_pack_dq_wps<M, 1>(a, cap, drop, s);
+  return launch_pack_dq_wps<M, 2>(a, cap, drop, s);
 }
 
 }  // namespace

@@ -199,6 +199,11 @@ def test_table_gradient_of_many_pairs(drop):
     assert e <= 5e-6
 
 
+@pytest.mark.parametrize("cap,drop", [(20.0, None), (None, DROP)])
+def test_wide_fp32_on_a_full_grid(cap, drop):
+    check("fp32 d=64, more workgroups than compute units", [400, 333, 260], 24, 64, 20, "f32", cap=cap, drop=drop)
+
+
 def test_many_small_graphs():
     g = np.random.default_rng(5)
     check("many small", [int(x) for x in g.integers(1, 50, 300)], 4, 8, 22, "bf16", cap=20.0, drop=DROP)
