@@ -201,7 +201,8 @@ def test_table_gradient_of_many_pairs(drop):
 
 @pytest.mark.parametrize("cap,drop", [(20.0, None), (None, DROP)])
 def test_wide_fp32_on_a_full_grid(cap, drop):
-    check("fp32 d=64, more workgroups than compute units", [400, 333, 260], 24, 64, 20, "f32", cap=cap, drop=drop)
+    _, pack, _ = check("fp32 d=64, more workgroups than compute units", [400, 333, 260], 40, 64, 20, "f32", cap=cap, drop=drop)
+    assert pack._info.jobs[1] * 40 > 256
 
 
 def test_many_small_graphs():
