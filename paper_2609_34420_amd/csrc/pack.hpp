@@ -603,8 +603,9 @@ inline int hist_buckets(int n_buckets) { return n_buckets < 32 ? 32 : (n_buckets
 // Workgroups of the one-pass backward of short graphs on a compute unit, by registers
 // and LDS: they are as many as fit, and take job after job.
 inline int hist_bytes(int n_buckets) { return hist_buckets(n_buckets) * (hist_buckets(n_buckets) == 256 ? 16 : 32) * 8; }
+constexpr int short_lds(int D, int blocks) { return 1024 + kPackWaves * (3 * 32 * D * 2 + blocks * 32 * 32 * 2 + 8); }
 inline int short_resident(int d, int blocks, bool cap, bool drop, int n_buckets) {
-  const int lds = (d == 64 ? 66592 : (blocks == 4 ? 58400 : 42016)) + hist_bytes(n_buckets);
+  const int lds = short_lds(d == 64 ? 64 : 32, blocks) + hist_bytes(n_buckets);
   const int by_lds = 160 * 1024 / lds, by_registers = d == 64 || blocks == 4 || (cap && drop) ? 2 : 3;
   return by_lds < by_registers ? by_lds : by_registers;
 }

@@ -49,6 +49,7 @@ __global__ __launch_bounds__(kPackThreads, NK == 2 && M::D == 32 && !(CAP && DRO
   __shared__ alignas(128) uint16_t sX[kPackWaves][NK][PT];
   __shared__ float red[kPackWaves];
   __shared__ int bad[kPackWaves];
+  static_assert(sizeof sTab + 3 * sizeof sK + sizeof sX + sizeof red + sizeof bad == short_lds(D, NK));
 
   const PackPlace pl(a, a.slots);
   if (pl.job >= a.slots) return;
@@ -288,26 +289,30 @@ __global__ __launch_bounds__(kPackThreads, NK == 2 && M::D == 32 && !(CAP && DRO
 template <class M, int NK, bool CAP, bool DROP>
 void launch_pack_short_nb(PackArgs a, hipStream_t s) {
   const dim3 grid(pack_grid(a.slots, a.H)), block(kPackThreads);
+  const int lds = hist_bytes(a.n_buckets);
   a.hist = hist_buckets(a.n_buckets);
-  if (a.hist == 256)
-    hipLaunchKernelGGL((pack_short_kernel<M, NK, CAP, DROP, true>), grid, block, hist_bytes(a.n_buckets), s, a);
-  else
-    hipLaunchKernelGGL((pack_short_kernel<M, NK, CAP, DROP, false>), grid, block, hist_bytes(a.n_buckets), s, a);
+  if constexpr (NK == 2) {
+    if (a.hist == 256) {
+      hipLaunchKernelGGL((pack_short_kernel<M, NK, CAP, DROP, true>), grid, block, lds, s, a);
+      return;
+    }
+  }
+  hipLaunchKernelGGL((pack_short_kernel<M, NK, CAP, DROP, false>), grid, block, lds, s, a);
 }
 
+// (NK = 4: without both cap and dropout and with fewer than 64 buckets, as its caller sees to)
 template <class M, int NK>
 hipError_t launch_pack_short(const PackArgs& a, bool cap, bool drop, hipStream_t s) {
+  if (NK == 4 && ((cap && drop) || a.n_buckets >= 64)) return hipErrorInvalidValue;
   if (cap && drop) {
-    if constexpr (NK == 2)
-      launch_pack_short_nb<M, NK, true, true>(a, s);
-    else
-      return hipErrorInvalidValue;                          // (such calls take two passes)
-  } else if (cap)
+    if constexpr (NK == 2) launch_pack_short_nb<M, NK, true, true>(a, s);
+  } else if (cap) {
     launch_pack_short_nb<M, NK, true, false>(a, s);
-  else if (drop)
+  } else if (drop) {
     launch_pack_short_nb<M, NK, false, true>(a, s);
-  else
+  } else {
     launch_pack_short_nb<M, NK, false, false>(a, s);
+  }
   return hipGetLastError();
 }
 
