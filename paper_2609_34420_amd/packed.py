@@ -261,6 +261,11 @@ def _on_stream(dev: int, stream, *held):
     return stream.cuda_stream
 
 
+def _like(x):
+    # (half the time of torch.empty with a shape; of another layout it would keep that)
+    return torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, device=x.device, dtype=x.dtype)
+
+
 def _launch(dev: int, fn, *args) -> int:
     # kernels are launched on the current device, which must be the tensors'
     if torch.cuda.current_device() == dev:
@@ -280,7 +285,7 @@ def gt_attn_pack_fwd(q, k, v, spd, table, pack: GTPack, scale: float | None = No
     drop = None if dropout is None else _dropout(dropout, dev)
     made = []
     if out is None:
-        out = torch.empty((H, T, d), device=q.device, dtype=dt)
+        out = _like(q)
         made.append(out)
     if lse is None:
         lse = torch.empty((H, T), device=q.device, dtype=torch.float32)
@@ -316,7 +321,7 @@ def gt_attn_pack_bwd(q, k, v, spd, table, pack: GTPack, o, lse, d_o, scale: floa
     _lse(lse, H, T)
     made = []
     if grads is None:
-        grads = made = [torch.empty(x.shape, device=q.device, dtype=x.dtype) for x in (q, k, v, table)]
+        grads = made = [_like(x) for x in (q, k, v, table)]
     elif len(grads) != 4:
         raise ValueError("grads must be (dq, dk, dv, dtable)")
     dq, dk, dv, dtable = grads
