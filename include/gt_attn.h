@@ -381,7 +381,7 @@ typedef struct {
   int32_t n_graphs, H;
   int32_t backward;            /* 0: the plan serves gt_attn_pack_fwd alone */
   /* internal: the kernels' work lists inside the plan */
-  int32_t jobs[3], merges, parts, slots, short_jobs, short_slots, short_blocks;
+  int32_t jobs[3], merges, parts, slots, slots3, short_jobs, short_slots, short_blocks;
   int64_t job_off[3], merge_off, short_off;
 } gt_attn_pack_t;
 

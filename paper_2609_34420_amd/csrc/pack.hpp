@@ -47,7 +47,7 @@ struct PackArgs {
   const PackWave* jobs;     // 4 per job
   int32_t njobs;
   int32_t slots;            // key-stationary: workgroups per head
-  int32_t hist;             // and buckets of its histogram, a power of two above n_buckets (256 at most)
+  int32_t hist;             // and buckets of its histogram, a power of two from n_buckets up
   const PackMerge* merges;
   int32_t nmerges;
   float* o_part;            // [slot, H, 32, d]
@@ -597,12 +597,20 @@ __device__ __forceinline__ void add_term(unsigned long long* at, float x) {
   }
 }
 
-// Buckets of the table gradient's histogram.
-inline int hist_buckets(int n_buckets) { return n_buckets < 32 ? 32 : (n_buckets < 64 ? 64 : (n_buckets < 128 ? 128 : 256)); }
+// Buckets of the table gradient's histogram, and its bytes: 32 copies and one more
+// bucket, or 16 copies of 256.
+inline int hist_buckets(int n_buckets) { return n_buckets <= 32 ? 32 : (n_buckets <= 64 ? 64 : (n_buckets <= 128 ? 128 : 256)); }
+inline int hist_bytes(int n_buckets) {
+  const int n = hist_buckets(n_buckets);
+  return n == 256 ? 256 * 16 * 8 : (n + 1) * 32 * 8;
+}
 
+// Workgroups of the bf16 dK / dV kernel on a compute unit.
+inline int dkdv_resident(int d, bool cap, bool drop, int n_buckets) {
+  return d <= 32 && !(cap && drop) && n_buckets <= 64 ? 3 : 2;
+}
 // Workgroups of the one-pass backward of short graphs on a compute unit, by registers
 // and LDS: they are as many as fit, and take job after job.
-inline int hist_bytes(int n_buckets) { return hist_buckets(n_buckets) * (hist_buckets(n_buckets) == 256 ? 16 : 32) * 8; }
 constexpr int short_lds(int D, int blocks) { return 1024 + kPackWaves * (3 * 32 * D * 2 + blocks * 32 * 32 * 2 + 8); }
 inline int short_resident(int d, int blocks, bool cap, bool drop, int n_buckets) {
   const int lds = short_lds(d == 64 ? 64 : 32, blocks) + hist_bytes(n_buckets);

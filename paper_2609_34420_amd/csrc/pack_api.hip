@@ -20,7 +20,8 @@ bool pack_ok(const gt_attn_pack_t* p) {
   if (!p || p->H < 1 || p->n_graphs < 1 || p->total_q < 0 || p->total_k < 0 || p->spd_bytes < 0) return false;
   for (int i = 0; i < 3; ++i)
     if (p->jobs[i] < 0 || p->job_off[i] < 0) return false;
-  return p->merges >= 0 && p->parts >= 0 && p->merge_off >= 0 && p->slots >= 0 && p->slots <= p->jobs[2] &&
+  return p->merges >= 0 && p->parts >= 0 && p->merge_off >= 0 && p->slots >= 0 && p->slots <= p->slots3 &&
+         p->slots3 <= p->jobs[2] &&
          p->short_jobs >= 0 && p->short_off >= 0 && p->short_slots >= 0 && p->short_slots <= p->short_jobs &&
          (p->short_blocks == 2 || p->short_blocks == 4);
 }
@@ -110,7 +111,7 @@ BwdParts bwd_parts(const gt_attn_pack_t* p, int32_t n_buckets) {
   BwdParts b;
   b.dmax = pad256(H * (size_t)p->total_q * sizeof(float));
   b.dtab = b.dmax + pad256(H * (size_t)p->jobs[1] * sizeof(float2));
-  const size_t slots = (size_t)(p->slots > p->short_slots ? p->slots : p->short_slots);
+  const size_t slots = (size_t)(p->slots3 > p->short_slots ? p->slots3 : p->short_slots);
   b.bytes = b.dtab + pad256(H * slots * (size_t)n_buckets * sizeof(double));
   return b;
 }
@@ -182,9 +183,9 @@ gt_status_t gt_attn_pack_bwd(const gt_attn_pack_t* pack, const void* plan, const
   a.d_o = gt::tensor(d_o); a.dq = gt::tensor(dq); a.dk = gt::tensor(dk); a.dv = gt::tensor(dv);
   a.dtable = dtable;
   a.njobs_dq = pack->jobs[1];
-  a.slots = pack->slots;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const bool bf16 = dtype == GT_BF16, c = cap > 0.0f, drop = a.thr > -32768;
+  a.slots = bf16 && gt::dkdv_resident(d, c, drop, n_buckets) == 3 ? pack->slots3 : pack->slots;
   hipError_t e = hipSuccess;
   if (bf16 && gt::short_applies(pack, d, c, drop, n_buckets)) {
     a.jobs = reinterpret_cast<const gt::PackWave*>(static_cast<const uint8_t*>(plan) + pack->short_off);

@@ -23,10 +23,9 @@
 // P and dU are rounded to bf16 as the operands of their products (2^-8 of a term).
 //
 // Bound: dependent chains (LDS reads, product, exponentials, product, LDS adds) at two
-// waves per SIMD, which the registers leave (253 of 256 at d = 64): vector units busy
+// waves per SIMD, which the registers leave at d = 64 (253 of 256): vector units busy
 // 62 %, LDS 19 % (16384 nodes, H = 8, d = 64, cap: 2050 to 2100 us, 530 TFLOP/s; without
-// the histogram's adds 1840). Three waves at d <= 32 spill: 37 against 33 us for 1024
-// graphs of 9 to 60 nodes. Two buffers of tiles at d = 64 spill too: 2180 against 2115.
+// the histogram's adds 1840). Two buffers of tiles spill: 2180 against 2115.
 #pragma once
 #include "pack.hpp"
 
@@ -49,14 +48,23 @@ __device__ __forceinline__ void transpose_bytes(uint8_t* st, int at, uint4 v, co
   }
 }
 
-// WIDE: more than 127 buckets (a narrow layout keeps its last bucket for the bytes
-// past it).
-template <class M, bool CAP, bool DROP, bool WIDE>
-__global__ __launch_bounds__(kPackThreads, M::BF16 || M::D < 64 ? 2 : 1) void pack_dkdv_kernel(PackArgs a) {
+// Three waves per SIMD: bf16 at d <= 32 but for cap and dropout together, whose registers
+// spill, with up to 64 buckets, more of which leave LDS for two workgroups. One buffer of
+// tiles then, two where two workgroups run (512 graphs of 100 to 256 nodes, d = 8,
+// dropout: 161 us with two waves, 142 with three; 16 graphs of up to 2400, d = 32, cap:
+// 133 and 126; 64 of 50 to 1000 with cap and dropout: 92 and 95).
+template <class M>
+constexpr bool three_waves(bool cap, bool drop) { return M::BF16 && M::D == 32 && !(cap && drop); }
+
+// BUCKETS: of the histogram's layout, up to 64, 128 or 256 (WIDE, which has an entry for
+// every byte; a narrow one has one more bucket for the bytes past it).
+template <class M, bool CAP, bool DROP, int BUCKETS>
+__global__ __launch_bounds__(kPackThreads, (three_waves<M>(CAP, DROP) && BUCKETS == 64 ? 3 : (M::BF16 || M::D < 64 ? 2 : 1)))
+void pack_dkdv_kernel(PackArgs a) {
   using T = typename M::T;
   constexpr int NA = M::NA;
-  // staged tiles: two where both fit beside the histogram twice per compute unit
-  constexpr int NB = M::BF16 && M::D == 32 ? 2 : 1;
+  constexpr bool WIDE = BUCKETS == 256;
+  constexpr int NB = M::BF16 && M::D == 32 && !(three_waves<M>(CAP, DROP) && BUCKETS == 64) ? 2 : 1;   // staged tiles
   constexpr int XCH = NA * 16 * 64 * 4 * 2;
   constexpr int STG = 2 * kPackWaves * M::TILE * (int)sizeof(T);
   constexpr int CPY = WIDE ? 16 : 32;
@@ -273,14 +281,14 @@ __global__ __launch_bounds__(kPackThreads, M::BF16 || M::D < 64 ? 2 : 1) void pa
         for (int r = 0; r < 16; ++r) x[r] = p[r] * dp[r];
       }
       if constexpr (!WIDE) {
-        // bytes past the layout go to its last bucket
+        // bytes past the layout go to a bucket behind it
         const uint32_t past = (0x100u - (uint32_t)a.hist) * 0x01010101u;
         if (__any(((b[0] | b[1] | b[2] | b[3]) & past) != 0)) {
 #pragma unroll
           for (int u = 0; u < 4; ++u)
 #pragma unroll
             for (int e = 0; e < 32; e += 8)
-              if ((b[u] & past) >> e & 0xffu) b[u] = (b[u] & ~(0xffu << e)) | (uint32_t)(a.hist - 1) << e;
+              if ((b[u] & past) >> e & 0xffu) b[u] = (b[u] & ~(0xffu << e)) | (uint32_t)a.hist << e;
         }
       }
       const uint32_t copy = (uint32_t)(lane & (CPY - 1)) * 8u;
@@ -404,11 +412,19 @@ __global__ __launch_bounds__(kPackThreads, M::BF16 || M::D < 64 ? 2 : 1) void pa
 template <class M, bool CAP, bool DROP>
 void launch_pack_dkdv_nb(PackArgs a, hipStream_t s) {
   const dim3 grid(pack_grid(a.slots, a.H)), block(kPackThreads);
+  const int lds = hist_bytes(a.n_buckets);
   a.hist = hist_buckets(a.n_buckets);
-  if (a.hist == 256)
-    hipLaunchKernelGGL((pack_dkdv_kernel<M, CAP, DROP, true>), grid, block, hist_bytes(a.n_buckets), s, a);
-  else
-    hipLaunchKernelGGL((pack_dkdv_kernel<M, CAP, DROP, false>), grid, block, hist_bytes(a.n_buckets), s, a);
+  if (a.hist == 256) {
+    hipLaunchKernelGGL((pack_dkdv_kernel<M, CAP, DROP, 256>), grid, block, lds, s, a);
+    return;
+  }
+  if constexpr (three_waves<M>(CAP, DROP)) {
+    if (a.hist <= 64) {
+      hipLaunchKernelGGL((pack_dkdv_kernel<M, CAP, DROP, 64>), grid, block, lds, s, a);
+      return;
+    }
+  }
+  hipLaunchKernelGGL((pack_dkdv_kernel<M, CAP, DROP, 128>), grid, block, lds, s, a);
 }
 
 template <class M>

@@ -236,12 +236,12 @@ class Plans {
 // other: the table, the histogram and its sums cost about as much as 16 blocks,
 // so short jobs share a workgroup as long as the chip stays full. Long ones get one
 // each, dealt out longest first as workgroups end.
-int32_t slots(const Plan& p, int32_t H) {
+int32_t slots(const Plan& p, int32_t H, int resident) {
   const int64_t n = (int64_t)p.jobs.size();
   int64_t sum = 0;
   for (const Job& j : p.jobs) sum += j.cost;
   const int64_t by_work = (sum + 15) / 16;
-  const int64_t full = (kSlots + H - 1) / H;
+  const int64_t full = (256 * resident + H - 1) / H;
   return (int32_t)std::min(n, std::max(by_work, full));
 }
 
@@ -323,7 +323,10 @@ gt_status_t make(int32_t G, int32_t H, const int32_t* n_q, const int32_t* n_k, c
       info.merges = (int32_t)p.merges.size();
       info.parts = p.parts;
     }
-    if (i == kDkdv) info.slots = slots(p, H);
+    if (i == kDkdv) {
+      info.slots = slots(p, H, 2);
+      info.slots3 = slots(p, H, 3);
+    }
   }
   std::vector<PackWave> shorts;
   info.short_blocks = 2;

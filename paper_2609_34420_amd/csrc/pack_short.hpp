@@ -207,14 +207,14 @@ __global__ __launch_bounds__(kPackThreads, NK == 2 && M::D == 32 && !(CAP && DRO
       if (kb * 32 >= lim1) continue;
       uint32_t (&b)[5] = w[kb];
       if constexpr (!WIDE) {
-        // bytes past the layout go to its last bucket
+        // bytes past the layout go to a bucket behind it
         const uint32_t past = (0x100u - (uint32_t)a.hist) * 0x01010101u;
         if (__any(((b[0] | b[1] | b[2] | b[3]) & past) != 0)) {
 #pragma unroll
           for (int u = 0; u < 4; ++u)
 #pragma unroll
             for (int e = 0; e < 32; e += 8)
-              if ((b[u] & past) >> e & 0xffu) b[u] = (b[u] & ~(0xffu << e)) | (uint32_t)(a.hist - 1) << e;
+              if ((b[u] & past) >> e & 0xffu) b[u] = (b[u] & ~(0xffu << e)) | (uint32_t)a.hist << e;
         }
       }
 #pragma unroll
@@ -300,10 +300,10 @@ void launch_pack_short_nb(PackArgs a, hipStream_t s) {
   hipLaunchKernelGGL((pack_short_kernel<M, NK, CAP, DROP, false>), grid, block, lds, s, a);
 }
 
-// (NK = 4: without both cap and dropout and with fewer than 64 buckets, as its caller sees to)
+// (NK = 4: without both cap and dropout and with up to 64 buckets, as its caller sees to)
 template <class M, int NK>
 hipError_t launch_pack_short(const PackArgs& a, bool cap, bool drop, hipStream_t s) {
-  if (NK == 4 && ((cap && drop) || a.n_buckets >= 64)) return hipErrorInvalidValue;
+  if (NK == 4 && ((cap && drop) || a.n_buckets > 64)) return hipErrorInvalidValue;
   if (cap && drop) {
     if constexpr (NK == 2) launch_pack_short_nb<M, NK, true, true>(a, s);
   } else if (cap) {

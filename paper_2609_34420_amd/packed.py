@@ -58,7 +58,7 @@ _Rows4, _Rows8 = _I64 * 12, _I64 * 24
 class _Info(ctypes.Structure):
     _fields_ = [("total_q", _I64), ("total_k", _I64), ("spd_bytes", _I64), ("plan_bytes", _I64),
                 ("n_graphs", _I32), ("H", _I32), ("backward", _I32), ("jobs", _I32 * 3), ("merges", _I32), ("parts", _I32),
-                ("slots", _I32), ("short_jobs", _I32), ("short_slots", _I32), ("short_blocks", _I32), ("job_off", _I64 * 3),
+                ("slots", _I32), ("slots3", _I32), ("short_jobs", _I32), ("short_slots", _I32), ("short_blocks", _I32), ("job_off", _I64 * 3),
                 ("merge_off", _I64), ("short_off", _I64)]
 
 

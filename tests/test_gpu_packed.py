@@ -205,6 +205,27 @@ def test_wide_fp32_on_a_full_grid(cap, drop):
     assert pack._info.jobs[1] * 40 > 256
 
 
+@pytest.mark.parametrize("cap,drop", [(None, None), (9.0, None), (None, DROP), (9.0, DROP)])
+@pytest.mark.parametrize("nb", [31, 32, 33, 63, 64, 65, 129])
+def test_bucket_layouts(nb, cap, drop):
+    """Buckets at the histogram's layouts' ends, with distances past the table and
+    past the layout, in batches of the two-pass and the one-pass backward."""
+    for n in ([150, 33], [60, 33]):
+        H, d = 2, 16
+        a = make(n, n, H, d, nb, "bf16", seed=22)
+        a["spd"][::7] = 255
+        a["spd"][3::7] = 129
+        r = upload(a)
+        pack = gt.gt_attn_pack(n, H, device=DEV)
+        args = (r["q"], r["k"], r["v"], r["spd"], r["table"], pack)
+        o, lse = gt.gt_attn_pack_fwd(*args, cap=cap, dropout=drop)
+        got = gt.gt_attn_pack_bwd(*args, o, lse, r["do"], cap=cap, dropout=drop)
+        torch.cuda.synchronize()
+        okw = dict(cap=cap or 0.0, dropout=drop and (drop.p, drop.seed, drop.offset))
+        want = oracle.packed_backward(a["q"], a["k"], a["v"], a["spd"], a["table"], d ** -0.5, a["do"], n, n, **okw)
+        compare(f"layout nb={nb} n={n}", "bf16", [o, lse, *got], [to_np(o), to_np(lse), *want])
+
+
 def test_many_small_graphs():
     g = np.random.default_rng(5)
     check("many small", [int(x) for x in g.integers(1, 50, 300)], 4, 8, 22, "bf16", cap=20.0, drop=DROP)
