@@ -91,6 +91,8 @@ class GTPack:
         self._plan = plan
         self._plan_at = plan.data_ptr()
         self._device_index = plan.get_device()
+        # the stream whose order the plan's memory goes by
+        self._stream = torch.cuda.current_stream(plan.device).cuda_stream if plan.is_cuda else 0
         self._ws = {}                                   # workspace sizes by what they depend on beside the plan
         self.total_q, self.total_k = info.total_q, info.total_k
         self.spd_bytes, self.H, self.n_graphs = info.spd_bytes, info.H, info.n_graphs
@@ -246,18 +248,23 @@ def _lse(lse, H: int, T: int):
         raise ValueError(f"lse must be a contiguous float32 tensor of shape ({H}, {T})")
 
 
-def _on_stream(dev: int, stream, *held):
+def _on_stream(dev: int, stream, pack: GTPack, made):
     """The raw stream of a call (dev's current one by default). What the call
-    allocated on the current stream, and the plan, are kept from reuse until a
-    stream of the caller's choice has passed it."""
+    allocated on the current stream, and the plan, which the caller does not see, are
+    kept from reuse until another stream that the call runs on has passed it."""
     cur = torch.cuda.current_stream(dev) if stream is not None or _raw_stream is None else None
     if stream is None:
-        return _raw_stream(dev) if cur is None else cur.cuda_stream
+        raw = _raw_stream(dev) if cur is None else cur.cuda_stream
+        if raw != pack._stream:
+            pack._plan.record_stream(torch.cuda.current_stream(dev))
+        return raw
     _need(stream.device_index == dev, "stream must be of the tensors' device")
     if stream.cuda_stream != cur.cuda_stream:
-        for t in held:
-            if t is not None and t.numel():
+        for t in made:
+            if t.numel():
                 t.record_stream(stream)
+    if stream.cuda_stream != pack._stream:
+        pack._plan.record_stream(stream)
     return stream.cuda_stream
 
 
@@ -301,7 +308,7 @@ def gt_attn_pack_fwd(q, k, v, spd, table, pack: GTPack, scale: float | None = No
     elif need:
         workspace = torch.empty(need, device=q.device, dtype=torch.uint8)
         made.append(workspace)
-    s = _on_stream(dev, stream, pack._plan, *made)
+    s = _on_stream(dev, stream, pack, made)
     st = _launch(dev, lib().gt_attn_pack_fwd, pack._at, pack._plan_at, at, at + _ROWS_BYTES, at + 2 * _ROWS_BYTES,
                  spd.data_ptr(), table.data_ptr(), table.shape[1], at + 3 * _ROWS_BYTES, lse.data_ptr(), T,
                  _ptr(workspace), 0 if workspace is None else workspace.numel(), d, _dt(q), scale, cap, drop, s)
@@ -342,7 +349,7 @@ def gt_attn_pack_bwd(q, k, v, spd, table, pack: GTPack, o, lse, d_o, scale: floa
     else:
         workspace = torch.empty(need, device=q.device, dtype=torch.uint8)
         made = [*made, workspace]
-    s = _on_stream(dev, stream, pack._plan, *made)
+    s = _on_stream(dev, stream, pack, made)
     st = _launch(dev, lib().gt_attn_pack_bwd, pack._at, pack._plan_at, at[0], at[1], at[2], spd.data_ptr(),
                  table.data_ptr(), nb, at[3], lse.data_ptr(), T, at[4], at[5], at[6], at[7], dtable.data_ptr(),
                  workspace.data_ptr(), workspace.numel(), d, _dt(q), scale, cap, drop, s)

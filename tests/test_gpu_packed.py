@@ -659,6 +659,31 @@ def test_streams_and_workspaces():
         gt.gt_attn_pack_bwd(*runs[0][0], *runs[0][2][:2], runs[0][1], workspace=ws[1][:need - 1])
 
 
+@pytest.mark.parametrize("how", ["current", "argument"])
+def test_plan_outlives_a_call_on_another_stream(how):
+    """A plan dropped while a side stream still has the call before it: its memory
+    is not handed out again until that stream has passed."""
+    n, H = [300, 45], 2
+    r = upload(make(n, n, H, 32, 22, "bf16", seed=23))
+    pack = gt.gt_attn_pack(n, H, device=DEV)
+    args = [r["q"], r["k"], r["v"], r["spd"], r["table"]]
+    want = gt.gt_attn_pack_fwd(*args, pack)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(50_000_000)
+        if how == "current":
+            got = gt.gt_attn_pack_fwd(*args, pack)
+    if how == "argument":
+        got = gt.gt_attn_pack_fwd(*args, pack, stream=side)
+    at, size = pack._plan.data_ptr(), pack._plan.untyped_storage().nbytes()
+    del pack
+    new = [torch.empty(size, dtype=torch.uint8, device=DEV) for _ in range(64)]
+    assert all(x.data_ptr() != at for x in new)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
 def test_agrees_with_the_unpacked_calls():
     """No option on: the packed call is the framework's attention of each graph."""
     n, H, d = [256, 77, 500], 2, 32
