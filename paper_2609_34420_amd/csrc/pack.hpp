@@ -556,14 +556,15 @@ struct PackSpdRow {
   const uint8_t* base;
   int range;
   uint32_t voff, sh;
-  // first: the wave's first row; rows: the query rows from there on (at least 1).
+  // first: the wave's first row; rows: the query rows from there on (at least 1);
+  // nk: the keys, 0 where there is nothing to read (all loads then give 0).
   __device__ __forceinline__ PackSpdRow(const uint8_t* first, int64_t ld, int64_t rows, int nk) {
     const int lane = threadIdx.x & 63;
     const int64_t n = rows < 32 ? rows : 32;
     const uint32_t rem = (uint32_t)(reinterpret_cast<uintptr_t>(first) & 15u);
     const int64_t i = (lane & 31) < n ? (lane & 31) : n - 1;
     base = uniform(first - rem);
-    range = uniform(rsrc_range(((n - 1) * ld + nk + rem + 3) & ~(int64_t)3));
+    range = uniform(rsrc_range(nk > 0 ? ((n - 1) * ld + nk + rem + 3) & ~(int64_t)3 : 0));
     voff = (uint32_t)(i * ld) + 16u * (uint32_t)(lane >> 5) + rem;
     sh = voff & 3u;
     voff -= sh;

@@ -297,8 +297,12 @@ gt_status_t make(int32_t G, int32_t H, const int32_t* n_q, const int32_t* n_k, c
       if (off > std::numeric_limits<int64_t>::max() - last) return GT_ERR_INVALID;
       info.spd_bytes = std::max(info.spd_bytes, off + last);
     }
+    // (a graph without pairs has no distances: the place and stride given for it, checked
+    // against no buffer, stay out of the records)
+    const bool pairs = a > 0 && b > 0;
     graphs.push_back({(int32_t)info.total_q, a, (int32_t)info.total_k, b,
-                      prefix ? prefix[g] : std::numeric_limits<int32_t>::max(), (int32_t)ld, off});
+                      prefix ? prefix[g] : std::numeric_limits<int32_t>::max(), pairs ? (int32_t)ld : b,
+                      pairs || !spd_off ? off : 0});
     info.total_q += a;
     info.total_k += b;
     if (info.total_q > std::numeric_limits<int32_t>::max() || info.total_k > std::numeric_limits<int32_t>::max())

@@ -20,7 +20,7 @@ struct PackWave {
   int32_t c0, c1;      // its group's columns [c0, c1), counted in the graph; c0 a multiple of 32
   int32_t prefix;      // key j is visible to query i if j < prefix or j <= i + nk - nq
   int64_t spd;         // byte offset of the graph's distances
-  int32_t ld;          // their row stride
+  int32_t ld;          // their row stride (nk in a graph without pairs)
   int32_t part;        // slot of a partial result, or -1
   int32_t log2w;
   int32_t combine;     // 1: the job's groups have the same rows; their results are added up
