@@ -1,7 +1,9 @@
 // dQ of packed attention (instantiated in pack_dq_*.hip), and the row sums
 // that the dK / dV kernel (pack_dkdv.hpp), launched after it, takes.
 //
-// Query-stationary as the forward: S^T = K Q^T, dP^T = V dO^T, P = exp(S - LSE),
+// Query-stationary as the forward: S^T = K Q^T, dP^T = V dO^T, P = exp(S - LSE)
+// at its own size before it meets dP (with the forward's reference of a head instead, and
+// LSE at the end, rows far below it lose dS of 2^-45, and those near it overflow at 2^60),
 //   dS = P (z dP / (1 - p) - D),   D_i = dO_i . O_i,
 //   dU = dS (1 - tanh^2),   dQ^T += K^T dU^T, times scale at the end.
 // D from a bf16 O is off by O's rounding: the table gradient, a sum in fp32, would
@@ -55,12 +57,10 @@ __global__ __launch_bounds__(kPackThreads, WPS) void pack_dq_kernel(PackArgs a) 
   const int lw = gr.log2w, W = 1 << lw;
   const int grp = wave >> lw, gw = wave & (W - 1);
   constexpr bool START = M::BF16 && !CAP;
-  ScoreRef ref{false, 0.0f};
-  if constexpr (M::BF16 && CAP) {
-    sTab[threadIdx.x] = capped_entry<M>(a, h, ref);
-  } else {
+  {
     const int b = threadIdx.x;
-    sTab[b] = M::entry(b < a.n_buckets ? a.table[(int64_t)h * a.n_buckets + b] : 0.0f, a, START);
+    sTab[b] = M::entry(b < a.n_buckets ? a.table[(int64_t)h * a.n_buckets + b] : 0.0f, a, START)
+              + (M::BF16 && CAP ? a.cap * kLog2e : 0.0f);
   }
 
   const int off = gr.nk - gr.nq;
@@ -126,10 +126,8 @@ __global__ __launch_bounds__(kPackThreads, WPS) void pack_dq_kernel(PackArgs a) 
       for (int r = 0; r < 16; ++r) x[r] = fmaf(s[r], sc.mul, mlse);
     } else {
       M::template scores<CAP, true>(s, x, slope, sc);
-      if (!ref.fixed) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) x[r] += mlse;
-      }
+      for (int r = 0; r < 16; ++r) x[r] += mlse;
     }
     if (j0 + 32 > lim0) keep_below(x, lim - j0 - 16 * g, -INFINITY);
     if constexpr (DROP) {
@@ -226,10 +224,7 @@ __global__ __launch_bounds__(kPackThreads, WPS) void pack_dq_kernel(PackArgs a) 
       blocks(sK0, sV0, 0, t0);
     }
   }
-  // with a fixed reference P = 2^x 2^(ref - LSE log2 e), the second factor taken here
-  const float pm = ref.fixed ? exp2_fast(ref.ref + mlse) : 1.0f;
-  dmax *= pm;
-  dsum = (dsum + __shfl_xor(dsum, 32)) * pm;
+  dsum += __shfl_xor(dsum, 32);
   dmax = wave_max(dmax);
   if (gr.combine) {
     float* stat = reinterpret_cast<float*>(sBuf0 + NA * 16 * 64 * 4 * 2) + lane;
@@ -247,7 +242,7 @@ __global__ __launch_bounds__(kPackThreads, WPS) void pack_dq_kernel(PackArgs a) 
   const float cmax = wave_max(mine ? fabsf(dsum) : 0.0f);
   if (lane == 0) sMax[wave] = make_float2(dmax, cmax);
   if (mine && iok) {
-    const float mul = a.scale * rp * pm * (CAP ? M::kSlope : 1.0f);
+    const float mul = a.scale * rp * (CAP ? M::kSlope : 1.0f);
     if constexpr (FIX) {
 #pragma unroll
       for (int c = 0; c < NA; ++c)
