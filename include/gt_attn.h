@@ -426,6 +426,9 @@ size_t gt_attn_pack_bwd_workspace_size(const gt_attn_pack_t* pack, int32_t n_buc
  *   lse    [H, ld_lse] fp32 (written), ld_lse >= total_q
  *   scale  2^-64 .. 2^64
  *   cap    0 (no cap), or in 2^-10 .. 2^10 (scores are off by up to about 2^-21 cap)
+ *          bf16 with a cap: the sums of P V carry a power of two per head, so O is finite
+ *          where |V| < 2^57 / n_k, and of rows whose scores all lie at the low end of the
+ *          cap and the table, values below 2^-35 lose bits
  *   dropout NULL: none
  * Otherwise as gt_attn_fwd. Deterministic. */
 gt_status_t gt_attn_pack_fwd(const gt_attn_pack_t* pack, const void* plan, const gt_attn_rows_t* q,

@@ -164,13 +164,15 @@ struct ScoreConst {
 };
 
 // Capped scores are bounded, and with them, table and all, the exponents: where
-// they span at most kSpan, the softmax needs no running reference but takes one for
-// the whole head, `ref`, kBelow below their top, which the table's entries carry:
-// no addition per score, no test per block, and no rescaling. exp stays within
-// 2^-110 .. 2^70, so sums of 2^25 keys and values up to 2^32 stay finite, and nothing
-// of a row whose scores are all at the low end underflows. (A cap of 50 spans 144;
-// 36 are left for the biases.)
-constexpr float kSpan = 180.0f, kBelow = 70.0f;
+// they span at most kSpan, the forward's softmax needs no running reference but takes
+// one for the whole head, `ref`, which the table's entries carry: no addition per
+// score, no test per block, and no rescaling. It is 0 where that keeps the exponents
+// within kTop - kSpan .. kTop (a table around 0), so that an entry is the backward's to
+// the last bit; else a whole number that does. exp stays within 2^-91 .. 2^70: sums over n
+// keys of values below 2^57 / n are finite, and of a row whose scores are all at the low end,
+// values from 2^-35 on keep all their bits. (A cap of 50 spans 144; 16 are left for the
+// biases.)
+constexpr float kSpan = 160.0f, kTop = 70.0f;
 struct ScoreRef {
   bool fixed;
   float ref;
@@ -209,8 +211,9 @@ __device__ __forceinline__ float capped_entry(const PackArgs& a, int h, ScoreRef
   hi = wave_max(hi);
   lo = -wave_max(-lo);
   r.fixed = hi >= lo && hi - lo + 2.0f * cap2 <= kSpan;      // (not if all entries are masks)
-  r.ref = r.fixed ? hi + cap2 - kBelow : 0.0f;
-  return own + (cap2 - r.ref);
+  const bool centred = hi + cap2 <= kTop && lo - cap2 >= kTop - kSpan;
+  r.ref = r.fixed && !centred ? ceilf(hi + cap2 - kTop) : 0.0f;
+  return (own + cap2) - r.ref;
 }
 
 // D: the tile's head dim (32 or 64); DS <= D: the tensors'.

@@ -83,3 +83,55 @@ def test_gradients_of_rows_far_below_the_table(dt, n, cap, spread):
                 assert err <= lim, (tag, name, g, err)
         err = rel_l2(to_np(got[3]), want[3] * 2.0 ** x)
         assert err <= LOW_F32, (tag, "dtable", err)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("drop", [None, DROP])
+@pytest.mark.parametrize("cap,spread", [(2.0, 100.0), (10.0, 85.0), (10.0, 89.0), (10.0, 93.0), (10.0, 100.0), (50.0, 0.0),
+                                        (50.0, 9.0), (50.0, 13.0)])
+def test_values_of_rows_far_below_the_table(dt, drop, cap, spread):
+    """Spans of the exponents up to a fixed reference's limit and past it (160 in base 2),
+    with V from 2^-60 to 2^48: each graph's rows by themselves. A cap of 50 adds 144 to the
+    152 of its spread at most, so LOW_F32 holds twice."""
+    n, H, d, nb = [70, 130, 90], 2, 32, 9
+    a = low_and_high(n, H, d, nb, dt, spread, seed=43)
+    r = upload(a)
+    pack = gt.gt_attn_pack(n, H, device=DEV)
+    want = oracle.packed_forward(a["q"], a["k"], a["v"], a["spd"], a["table"], d ** -0.5, n, n, cap=cap,
+                                 dropout=drop and (drop.p, drop.seed, drop.offset))
+    e = np.cumsum([0, *n])
+    for x in (0, -60, 48):
+        tag = f"values {dt} cap={cap} spread={spread} drop={drop is not None} V 2^{x}"
+        say(tag)
+        o, lse = gt.gt_attn_pack_fwd(r["q"], r["k"], r["v"] * 2.0 ** x, r["spd"], r["table"], pack, cap=cap, dropout=drop)
+        torch.cuda.synchronize()
+        for g in range(3):
+            at = slice(e[g], e[g + 1])
+            err = rel_l2(to_np(o[:, at]), want[0][:, at] * 2.0 ** x)
+            assert err <= (TOL["bf16"]["o"] if dt == "bf16" else 2 * LOW_F32), (tag, g, err)
+            assert rel_l2(to_np(lse[:, at]), want[1][:, at]) <= 2 * LOW_F32, (tag, g)
+
+
+def test_capped_scores_are_the_backwards():
+    """Small graphs with a cap of 20, bf16: forward and backward round their entries alike.
+    A capped score in base 2 (terms of up to 2 cap log2 e = 58) is then off by the reciprocal, a
+    step of 2^-24 at most, times 58, by the exponential's step of 2^-23 times 58 / 4, and by the
+    entry's half step at 29, 2^-20: as uniform errors 2.0, 1.0 and 0.55e-6 in root mean square,
+    2.3e-6 in all, 1.6e-6 of P. A sum of independent terms is off by as much of itself: 3e-6 with
+    the LSE's. The LSE is rounded three times, 3 * 2^-24, and carries less than a fourth of
+    a score's error: 3e-7 of some 5."""
+    g = np.random.default_rng(44)
+    n, H, d, nb = [int(x) for x in g.integers(9, 61, 200)], 4, 8, 22
+    a = make(n, n, H, d, nb, "bf16", seed=44, gain=2.0)
+    r = upload(a)
+    pack = gt.gt_attn_pack(n, H, device=DEV)
+    args = (r["q"], r["k"], r["v"], r["spd"], r["table"], pack)
+    o, lse = gt.gt_attn_pack_fwd(*args, cap=20.0)
+    dt = gt.gt_attn_pack_bwd(*args, o, lse, r["do"], cap=20.0)[3]
+    torch.cuda.synchronize()
+    kw = dict(cap=20.0)
+    want = (oracle.packed_forward(a["q"], a["k"], a["v"], a["spd"], a["table"], d ** -0.5, n, n, **kw)[1],
+            oracle.packed_backward(a["q"], a["k"], a["v"], a["spd"], a["table"], d ** -0.5, a["do"], n, n, **kw)[3])
+    el, et = rel_l2(to_np(lse), want[0]), rel_l2(to_np(dt), want[1])
+    say(f"capped small graphs: LSE {el:.2e} dtable {et:.2e}")
+    assert el <= 3e-7 and et <= 3e-6
