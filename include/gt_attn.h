@@ -399,8 +399,8 @@ typedef struct {
  *   n_q, n_k  [n_graphs] rows, 0 allowed, at most 2^25 - 16
  *   prefix    [n_graphs] >= 0, or NULL: no prefix mask
  *   spd_off, spd_ld  [n_graphs] byte offset of a graph's [n_q, n_k] distances and
- *             their row stride (n_k .. 2^25 - 16), or NULL: the matrices lie dense, one
- *             behind the other. A graph without queries or without keys has no distances:
+ *             their row stride (n_k .. 2^25 - 16), or NULL: the rows lie dense, and the
+ *             matrices, n_q rows of the stride each, one behind the other. A graph without queries or without keys has no distances:
  *             nothing is read from the place given for it
  *   backward  0: without the backward's work lists, for evaluation and serving (they are
  *             most of a plan where a few rows meet many keys)

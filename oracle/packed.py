@@ -104,7 +104,7 @@ def _walk(n_q, n_k, spd, spd_off, spd_ld):
         else:
             m = np.zeros((x, y), np.uint8)
         yield g, slice(a, a + x), slice(b, b + y), m
-        a, b, s = a + x, b + y, s + x * y
+        a, b, s = a + x, b + y, s + x * ld
 
 
 def packed_forward(q, k, v, spd, table, scale, n_q, n_k, cap=0.0, prefix=None, dropout=None, spd_off=None, spd_ld=None):

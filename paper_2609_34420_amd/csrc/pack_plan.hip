@@ -281,17 +281,17 @@ gt_status_t make(int32_t G, int32_t H, const int32_t* n_q, const int32_t* n_k, c
   std::vector<Graph> graphs;
   graphs.reserve(G);
   gt_attn_pack_t info{};
-  int64_t dense = 0;
+  int64_t behind = 0;                    // byte behind the graphs so far, one behind the other
   for (int32_t g = 0; g < G; ++g) {
     const int32_t a = n_q[g], b = n_k[g];
     if (a < 0 || b < 0) return GT_ERR_INVALID;
     if (a > kMaxNodes || b > kMaxNodes) return GT_ERR_UNSUPPORTED;
     if (prefix && prefix[g] < 0) return GT_ERR_INVALID;
     const int64_t ld = spd_ld ? spd_ld[g] : b;
-    const int64_t off = spd_off ? spd_off[g] : dense;
+    const int64_t off = spd_off ? spd_off[g] : behind;
     if (ld < b || off < 0) return GT_ERR_INVALID;
     if (ld > kMaxNodes) return GT_ERR_UNSUPPORTED;
-    dense += (int64_t)a * b;
+    behind += (int64_t)a * ld;
     if (a > 0 && b > 0) {
       const int64_t last = (int64_t)(a - 1) * ld + b;
       if (off > std::numeric_limits<int64_t>::max() - last) return GT_ERR_INVALID;
@@ -302,7 +302,7 @@ gt_status_t make(int32_t G, int32_t H, const int32_t* n_q, const int32_t* n_k, c
     const bool pairs = a > 0 && b > 0;
     graphs.push_back({(int32_t)info.total_q, a, (int32_t)info.total_k, b,
                       prefix ? prefix[g] : std::numeric_limits<int32_t>::max(), pairs ? (int32_t)ld : b,
-                      pairs || !spd_off ? off : 0});
+                      pairs || !(spd_off || spd_ld) ? off : 0});
     info.total_q += a;
     info.total_k += b;
     if (info.total_q > std::numeric_limits<int32_t>::max() || info.total_k > std::numeric_limits<int32_t>::max())

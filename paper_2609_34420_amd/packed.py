@@ -115,8 +115,9 @@ def gt_attn_pack(n_q, H: int, n_k=None, prefix=None, spd_off=None, spd_ld=None, 
     """The plan of a packed batch (C ABI gt_attn_pack_plan) for graphs of n_q[g]
     query rows and n_k[g] keys (n_q by default) and H heads. prefix: None, or the
     number of leading keys that every row of a graph sees beside those up to its own
-    position (0: causal). spd_off, spd_ld: where a graph's distances lie in spd and
-    their row stride, where they are not dense, one matrix behind the other.
+    position (0: causal). spd_off, spd_ld: where a graph's distances lie in spd (by
+    default one matrix of n_q[g] rows of the stride behind the other) and their row
+    stride (n_k[g]).
     backward=False: a plan for the forward alone, sooner made where a few rows meet
     many keys (the new nodes of 16 graphs of 1000 to 16000: 45 us for 215). Made
     once per batch of sizes, it serves every layer's and step's calls; a captured

@@ -135,3 +135,21 @@ def test_capped_scores_are_the_backwards():
     el, et = rel_l2(to_np(lse), want[0]), rel_l2(to_np(dt), want[1])
     say(f"capped small graphs: LSE {el:.2e} dtable {et:.2e}")
     assert el <= 3e-7 and et <= 3e-6
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_padded_distances_one_behind_the_other(dt):
+    n, ld, H = [70, 33, 0, 150], [80, 33, 16, 153], 2
+    r = upload(make(n, n, H, 32, 22, dt, seed=45))
+    padded = torch.full((sum(x * y for x, y in zip(n, ld)),), 255, dtype=torch.uint8, device=DEV)
+    s = t = 0
+    for x, y in zip(n, ld):
+        padded[t:t + x * y].view(x, y)[:, :x] = r["spd"][s:s + x * x].view(x, x)
+        s, t = s + x * x, t + x * y
+    got = []
+    for spd, kw in ((r["spd"], {}), (padded, dict(spd_ld=ld))):
+        args = (r["q"], r["k"], r["v"], spd, r["table"], gt.gt_attn_pack(n, H, device=DEV, **kw))
+        o, lse = gt.gt_attn_pack_fwd(*args, cap=9.0)
+        got.append((o, lse, *gt.gt_attn_pack_bwd(*args, o, lse, r["do"], cap=9.0)))
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(*got))
