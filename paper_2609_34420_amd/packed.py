@@ -249,24 +249,29 @@ def _lse(lse, H: int, T: int):
         raise ValueError(f"lse must be a contiguous float32 tensor of shape ({H}, {T})")
 
 
-def _on_stream(dev: int, stream, pack: GTPack, made):
-    """The raw stream of a call (dev's current one by default). What the call
-    allocated on the current stream, and the plan, which the caller does not see, are
-    kept from reuse until another stream that the call runs on has passed it."""
-    cur = torch.cuda.current_stream(dev) if stream is not None or _raw_stream is None else None
-    if stream is None:
-        raw = _raw_stream(dev) if cur is None else cur.cuda_stream
-        if raw != pack._stream:
-            pack._plan.record_stream(torch.cuda.current_stream(dev))
-        return raw
-    _need(stream.device_index == dev, "stream must be of the tensors' device")
-    if stream.cuda_stream != cur.cuda_stream:
-        for t in made:
-            if t.numel():
-                t.record_stream(stream)
-    if stream.cuda_stream != pack._stream:
-        pack._plan.record_stream(stream)
-    return stream.cuda_stream
+def _on_stream(stream, q, given, call):
+    """call() with `stream` as the current one, so that what it allocates (the results
+    whose place in `given` is None, and a workspace) is that stream's memory: a block of
+    another's may have work pending there. The results are kept from reuse until the
+    caller's current stream, where they go next, has passed them too."""
+    if isinstance(q, torch.Tensor) and stream.device_index != q.get_device():
+        raise ValueError("stream must be of the tensors' device")
+    cur = torch.cuda.current_stream(stream.device)
+    with torch.cuda.stream(stream):
+        got = call()
+    for t, g in zip(got, given):
+        if g is None and t.numel():
+            t.record_stream(cur)
+    return got
+
+
+def _current(dev: int, pack: GTPack) -> int:
+    """The raw current stream. The plan, which the caller does not see, is kept from
+    reuse until a stream other than its own has passed the call."""
+    raw = _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream(dev).cuda_stream
+    if raw != pack._stream:
+        pack._plan.record_stream(torch.cuda.current_stream(dev))
+    return raw
 
 
 def _like(x):
@@ -287,17 +292,18 @@ def gt_attn_pack_fwd(q, k, v, spd, table, pack: GTPack, scale: float | None = No
     """O [H, T, d] (q's type) and LSE [H, T] fp32 of the packed batch (C ABI
     gt_attn_pack_fwd). cap: bound of the scores before the bias, None for none;
     dropout: GTDropout or None. Rows behind the batch's total stay as they are
-    (uninitialised where the call allocates)."""
+    (uninitialised where the call allocates). stream: as if it were the current one; the
+    caller orders it with the streams of what is passed in."""
+    if stream is not None:
+        return _on_stream(stream, q, (out, lse), lambda: gt_attn_pack_fwd(
+            q, k, v, spd, table, pack, scale, cap, dropout, out, lse, workspace))
     dt, H, d, dev, rows, scale, cap = _common(q, k, v, spd, table, pack, scale, cap)
     T = q.shape[1]
     drop = None if dropout is None else _dropout(dropout, dev)
-    made = []
     if out is None:
         out = _like(q)
-        made.append(out)
     if lse is None:
         lse = torch.empty((H, T), device=q.device, dtype=torch.float32)
-        made.append(lse)
     else:
         _lse(lse, H, T)
         _same_device(dev, lse)
@@ -308,8 +314,7 @@ def gt_attn_pack_fwd(q, k, v, spd, table, pack: GTPack, scale: float | None = No
         _workspace(workspace, need, q)
     elif need:
         workspace = torch.empty(need, device=q.device, dtype=torch.uint8)
-        made.append(workspace)
-    s = _on_stream(dev, stream, pack, made)
+    s = _current(dev, pack)
     st = _launch(dev, lib().gt_attn_pack_fwd, pack._at, pack._plan_at, at, at + _ROWS_BYTES, at + 2 * _ROWS_BYTES,
                  spd.data_ptr(), table.data_ptr(), table.shape[1], at + 3 * _ROWS_BYTES, lse.data_ptr(), T,
                  _ptr(workspace), 0 if workspace is None else workspace.numel(), d, _dt(q), scale, cap, drop, s)
@@ -322,14 +327,17 @@ def gt_attn_pack_bwd(q, k, v, spd, table, pack: GTPack, o, lse, d_o, scale: floa
                      stream=None):
     """dQ, dK, dV and dTable of the packed batch (C ABI gt_attn_pack_bwd), with
     the forward's arguments and results. `grads` may hold preallocated (dq, dk,
-    dv, dtable); rows behind the batch's totals stay as they are."""
+    dv, dtable); rows behind the batch's totals stay as they are. stream: as the
+    forward's."""
+    if stream is not None:
+        return _on_stream(stream, q, grads or [None] * 4, lambda: gt_attn_pack_bwd(
+            q, k, v, spd, table, pack, o, lse, d_o, scale, cap, dropout, workspace, grads))
     dt, H, d, dev, rows, scale, cap = _common(q, k, v, spd, table, pack, scale, cap)
     T, nb = q.shape[1], table.shape[1]
     drop = None if dropout is None else _dropout(dropout, dev)
     _lse(lse, H, T)
-    made = []
     if grads is None:
-        grads = made = [_like(x) for x in (q, k, v, table)]
+        grads = [_like(x) for x in (q, k, v, table)]
     elif len(grads) != 4:
         raise ValueError("grads must be (dq, dk, dv, dtable)")
     dq, dk, dv, dtable = grads
@@ -349,8 +357,7 @@ def gt_attn_pack_bwd(q, k, v, spd, table, pack: GTPack, o, lse, d_o, scale: floa
         _workspace(workspace, need, q)
     else:
         workspace = torch.empty(need, device=q.device, dtype=torch.uint8)
-        made = [*made, workspace]
-    s = _on_stream(dev, stream, pack, made)
+    s = _current(dev, pack)
     st = _launch(dev, lib().gt_attn_pack_bwd, pack._at, pack._plan_at, at[0], at[1], at[2], spd.data_ptr(),
                  table.data_ptr(), nb, at[3], lse.data_ptr(), T, at[4], at[5], at[6], at[7], dtable.data_ptr(),
                  workspace.data_ptr(), workspace.numel(), d, _dt(q), scale, cap, drop, s)
