@@ -2,7 +2,9 @@
 
 Thin Python binding of libgtattn.so. Every function here only marshals
 arguments: it checks tensors, allocates outputs with torch (device memory
-only) and calls the C ABI of the same name on the current HIP stream. All
+only) and calls the C ABI of the same name on the current HIP stream, or on
+`stream` where a call is given one: what it allocates is then memory of that
+stream, and the caller orders it with the streams of the inputs. All
 computation runs in the library's HIP kernels; there is no fallback path.
 If the library is missing or cannot be loaded, every call raises.
 
@@ -142,6 +144,20 @@ def _stream(stream) -> int | None:
     return stream.cuda_stream
 
 
+def _made(stream, make, *a, **kw):
+    """A tensor that a call allocates: memory of the stream that the call runs on (a
+    block of another's may have work pending there), kept from reuse until the caller's
+    current stream, where a result goes next, has passed it too."""
+    if stream is None:
+        return make(*a, **kw)
+    cur = torch.cuda.current_stream(stream.device)
+    with torch.cuda.stream(stream):
+        t = make(*a, **kw)
+    if t.numel():
+        t.record_stream(cur)
+    return t
+
+
 def _check(status: int, what: str):
     if status != 0:
         raise GTError(status, what)
@@ -241,9 +257,9 @@ def gt_attn_fwd(q, k, v, spd, table, scale: float | None = None, out=None, lse=N
     _devices(q, k, v, spd, table, out, lse)
     scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
     if out is None:
-        out = torch.empty_like(q)
+        out = _made(stream, torch.empty_like, q)
     if lse is None:
-        lse = torch.empty((H, N), device=q.device, dtype=torch.float32)
+        lse = _made(stream, torch.empty, (H, N), device=q.device, dtype=torch.float32)
     st = lib().gt_attn_fwd(_ptr(q), _ptr(k), _ptr(v), _ptr(spd), _ptr(table), table.shape[1],
                            _ptr(out), _ptr(lse), H, N, d, _dt(q), scale, _stream(stream))
     _check(st, "gt_attn_fwd")
@@ -301,11 +317,10 @@ def gt_attn_bwd_phase(phase: int, q, k, v, spd, table, o, lse, d_o, scale: float
         _workspace(workspace, need, q)
     scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
     if grads is None:
-        grads = (torch.empty_like(q), torch.empty_like(k), torch.empty_like(v),
-                 torch.empty_like(table))
+        grads = tuple(_made(stream, torch.empty_like, t) for t in (q, k, v, table))
     dq, dk, dv, dtable = grads
     if workspace is None:
-        workspace = torch.empty(need, device=q.device, dtype=torch.uint8)
+        workspace = _made(stream, torch.empty, need, device=q.device, dtype=torch.uint8)
     args = (_ptr(q), _ptr(k), _ptr(v), _ptr(spd), None if spd_t is None else _ptr(spd_t),
             _ptr(table), table.shape[1],
             _ptr(o), _ptr(lse), _ptr(d_o), _ptr(dq), _ptr(dk), _ptr(dv),
@@ -370,9 +385,9 @@ def gt_attn_fwd_batch(q, k, v, spd, table, scale: float | None = None, out=None,
     _devices(q, k, v, spd, table, out, lse)
     scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
     if out is None:
-        out = torch.empty_like(q)
+        out = _made(stream, torch.empty_like, q)
     if lse is None:
-        lse = torch.empty((B, H, N), device=q.device, dtype=torch.float32)
+        lse = _made(stream, torch.empty, (B, H, N), device=q.device, dtype=torch.float32)
     st = lib().gt_attn_fwd_batch(_ptr(q), _ptr(k), _ptr(v), _ptr(spd), stride, _ptr(table),
                                  table.shape[1], _ptr(out), _ptr(lse), B, H, N, d, _dt(q), scale,
                                  _stream(stream))
@@ -394,11 +409,10 @@ def gt_attn_bwd_batch(q, k, v, spd, table, o, lse, d_o, scale: float | None = No
         _workspace(workspace, need, q)
     scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
     if grads is None:
-        grads = (torch.empty_like(q), torch.empty_like(k), torch.empty_like(v),
-                 torch.empty_like(table))
+        grads = tuple(_made(stream, torch.empty_like, t) for t in (q, k, v, table))
     dq, dk, dv, dtable = grads
     if workspace is None:
-        workspace = torch.empty(need, device=q.device, dtype=torch.uint8)
+        workspace = _made(stream, torch.empty, need, device=q.device, dtype=torch.uint8)
     st = lib().gt_attn_bwd_batch(_ptr(q), _ptr(k), _ptr(v), _ptr(spd),
                                  None if spd_t is None else _ptr(spd_t), stride, _ptr(table),
                                  table.shape[1], _ptr(o), _ptr(lse), _ptr(d_o), _ptr(dq), _ptr(dk),
@@ -444,9 +458,9 @@ def gt_attn_ring_step(q_shard, k_shard, v_shard, spd, row_off: int, col_off: int
         _devices(q_shard, spd, contiguous=False)
     scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
     if out is None:
-        out = torch.empty((H, Sq, d), device=q_shard.device, dtype=torch.float32)
+        out = _made(stream, torch.empty, (H, Sq, d), device=q_shard.device, dtype=torch.float32)
     if lse is None:
-        lse = torch.empty((H, Sq), device=q_shard.device, dtype=torch.float32)
+        lse = _made(stream, torch.empty, (H, Sq), device=q_shard.device, dtype=torch.float32)
     ld = spd.stride(0) if (spd is not None and Sk > 0) else 0
     st = lib().gt_attn_ring_step(_ptr(q_shard), Sq, _ptr(k_shard), _ptr(v_shard), Sk,
                                  _ptr(spd) if Sk > 0 else None, ld, int(row_off), int(col_off),
@@ -523,13 +537,11 @@ def gt_attn_bwd_ring_step(q_shard, o_shard, lse_shard, d_o_shard, k_blk, v_blk, 
     scale = 1.0 / math.sqrt(d) if scale is None else float(scale)
     dev = q_shard.device
     if acc is None:
-        acc = (torch.zeros((H, Sq, d), device=dev, dtype=torch.float32),
-               torch.zeros((H, Sk, d), device=dev, dtype=torch.float32),
-               torch.zeros((H, Sk, d), device=dev, dtype=torch.float32),
-               torch.zeros_like(table))
+        acc = tuple(_made(stream, torch.zeros, s, device=dev, dtype=torch.float32)
+                    for s in ((H, Sq, d), (H, Sk, d), (H, Sk, d), table.shape))
     dq, dk, dv, dtable = acc
     if workspace is None:
-        workspace = torch.empty(max(need, 1), device=dev, dtype=torch.uint8)
+        workspace = _made(stream, torch.empty, max(need, 1), device=dev, dtype=torch.uint8)
     ld = spd.stride(0) if (spd is not None and Sk > 0) else 0
     st = lib().gt_attn_bwd_ring_step(
         _ptr(q_shard), _ptr(o_shard), _ptr(lse_shard), _ptr(d_o_shard), Sq,
@@ -558,9 +570,9 @@ def gt_attn_merge(o_parts, lse_parts, dtype=torch.bfloat16, out=None, lse=None, 
         _shape(lse, "lse", (H, S), torch.float32)
     _devices(o_parts, lse_parts, out, lse)
     if out is None:
-        out = torch.empty((H, S, d), device=o_parts.device, dtype=dtype)
+        out = _made(stream, torch.empty, (H, S, d), device=o_parts.device, dtype=dtype)
     if lse is None:
-        lse = torch.empty((H, S), device=o_parts.device, dtype=torch.float32)
+        lse = _made(stream, torch.empty, (H, S), device=o_parts.device, dtype=torch.float32)
     st = lib().gt_attn_merge(_ptr(o_parts), _ptr(lse_parts), P, _ptr(out), _ptr(lse), H, S, d,
                              GT_BF16 if out.dtype == torch.bfloat16 else GT_F32, _stream(stream))
     _check(st, "gt_attn_merge")

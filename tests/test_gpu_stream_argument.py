@@ -27,7 +27,36 @@ def new_nodes(seed):
     return {"pack_parts": lambda s: gt.gt_attn_pack_fwd(r["q"], r["k"], r["v"], r["spd"], r["table"], pack, stream=s)}
 
 
-CALLS = {"pack_fwd": packed, "pack_bwd": packed, "pack_parts": new_nodes}
+def unpacked(seed):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    B, H, N, d = 3, 2, 320, 32
+    q, k, v, do = (torch.randn(B, H, N, d, device=DEV, generator=g).bfloat16() for _ in range(4))
+    spd = torch.randint(0, 22, (N, N), device=DEV, generator=g, dtype=torch.uint8)
+    t = torch.randn(H, 22, device=DEV, generator=g)
+    one, parts = (q[0], k[0], v[0], spd, t), torch.randn(4, H, N, d, device=DEV, generator=g)
+    lses = torch.randn(4, H, N, device=DEV, generator=g)
+    f, fb = gt.gt_attn_fwd(*one), gt.gt_attn_fwd_batch(q, k, v, spd, t)
+    return {"fwd": lambda s: gt.gt_attn_fwd(*one, stream=s),
+            "bwd": lambda s: gt.gt_attn_bwd(*one, *f, do[0], stream=s),
+            "fwd_batch": lambda s: gt.gt_attn_fwd_batch(q, k, v, spd, t, stream=s),
+            "bwd_batch": lambda s: gt.gt_attn_bwd_batch(q, k, v, spd, t, *fb, do, stream=s),
+            "ring_step": lambda s: gt.gt_attn_ring_step(q[0], k[0], v[0], spd, 0, 0, t, stream=s),
+            "bwd_ring_step": lambda s: gt.gt_attn_bwd_ring_step(q[0], *f, do[0], k[0], v[0], spd, 0, 0, t, stream=s),
+            "merge": lambda s: gt.gt_attn_merge(parts, lses, stream=s)}
+
+
+CALLS = {"pack_fwd": packed, "pack_bwd": packed, "pack_parts": new_nodes,
+         **{n: unpacked for n in ("fwd", "bwd", "fwd_batch", "bwd_batch", "ring_step", "bwd_ring_step", "merge")}}
+
+
+def same(name, got, want):
+    """Bit by bit; the unpacked backward's fp32 sums over workgroups are atomics, whose order
+    varies: some 30 additions, each off by half a step of 2^-24 of partial sums up to five
+    times the result, 1e-5 of it."""
+    loose = name.startswith("bwd")
+    return all(torch.equal(x, y) or (loose and y.dtype == torch.float32
+                                     and float((x - y).double().norm()) <= 1e-5 * float(y.double().norm()))
+               for x, y in zip(got, want))
 
 
 def fill_pending(tensors):
@@ -49,9 +78,9 @@ def test_memory_has_nothing_pending(name):
     fill_pending(want)
     got = call(side)
     side.synchronize()
-    assert all(torch.equal(x.cpu(), y.cpu()) for x, y in zip(got, want))
+    assert same(name, [x.cpu() for x in got], [y.cpu() for y in want])
     torch.cuda.synchronize()
-    assert all(torch.equal(x, y) for x, y in zip(got, want))
+    assert same(name, got, want)
 
 
 @pytest.mark.parametrize("name", CALLS)
@@ -70,7 +99,7 @@ def test_results_outlive_the_callers_use(name):
     for _ in range(3):
         other(side)
     torch.cuda.synchronize()
-    assert all(torch.equal(x, y) for x, y in zip(copies, want))
+    assert same(name, copies, want)
 
 
 @pytest.mark.parametrize("name", CALLS)
@@ -88,6 +117,6 @@ def test_captured_on_a_forked_stream(name):
     for _ in range(3):
         graph.replay()
         torch.cuda.synchronize()
-        assert all(torch.equal(x, y) for x, y in zip(got, want))
+        assert same(name, got, want)
         call(None)
         torch.cuda.synchronize()
