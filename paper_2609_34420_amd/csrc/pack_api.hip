@@ -87,12 +87,15 @@ void stage(const gt_attn_pack_t* pack, const void* plan, int i, PackArgs& a) {
   a.njobs = pack->jobs[i];
 }
 
-// The one-pass backward: faster than two passes wherever it was measured with up to two
-// blocks of keys (1024 graphs of 9 to 60 nodes, d = 8: 33 and 55 us; 300 of 40 to 64, d =
-// 64, cap and dropout: 43 and 80), and with up to four if two workgroups fit a compute
-// unit (2048 graphs of 85 to 92, d = 16, 22 buckets, cap: 310 and 401; 512 of 65 to 128,
-// d = 8, 64 buckets, of which one fits: 136 and 125) and not both a cap and dropout
-// take registers (2048 of 85 to 92: 466 and 470).
+// The one-pass backward: faster than two passes wherever it was measured (H = 8, the whole
+// call, one pass and two). With up to two blocks of keys 1024 graphs of 9 to 60 nodes, d = 8,
+// cap: 41 and 63 us; 300 of 40 to 64, d = 64, cap and dropout: 43 and 79; 2048 of 16 to 40,
+// d = 64, 256 buckets, of which one workgroup fits a compute unit: 185 and 238. With up to
+// four where two workgroups fit, up to 64 buckets: of 156 batches of 65 to 128 nodes or with
+// one such graph the least gain is 2048 of 65 to 96, d = 8, 64 buckets: 233 and 252; 1024 of
+// 100 to 128, d = 32, cap: 222 and 293. One workgroup of those to a unit lost (512 of 65 to
+// 128, d = 8: 136 and 125), and a cap and dropout together, which take registers, gained
+// nothing (2048 of 85 to 92: 466 and 470).
 bool short_applies(const gt_attn_pack_t* p, int32_t d, bool cap, bool drop, int32_t n_buckets) {
   return p->short_jobs > 0 &&
          (p->short_blocks == 2 ||
