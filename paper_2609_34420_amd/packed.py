@@ -99,6 +99,17 @@ class GTPack:
         self.backward = bool(info.backward)
         self.device = plan.device
 
+    # (a plan holds addresses: a copy of its attributes would keep those of the original)
+    def __copy__(self):
+        return self
+
+    def __reduce__(self):
+        return _copied_pack, (bytes(self._info), self._plan)
+
+
+def _copied_pack(info: bytes, plan: torch.Tensor) -> GTPack:
+    return GTPack(_Info.from_buffer_copy(info), plan)
+
 
 def _sizes(x, name: str, n: int | None, dtype=np.int32) -> np.ndarray:
     a = np.asarray(x)

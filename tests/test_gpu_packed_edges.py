@@ -1,5 +1,5 @@
 """Packed attention at the edges of what its documentation allows."""
-import math
+import copy
 
 import numpy as np
 import pytest
@@ -153,3 +153,36 @@ def test_padded_distances_one_behind_the_other(dt):
         got.append((o, lse, *gt.gt_attn_pack_bwd(*args, o, lse, r["do"], cap=9.0)))
     torch.cuda.synchronize()
     assert all(torch.equal(x, y) for x, y in zip(*got))
+
+
+def test_a_copied_plan():
+    n, H = [70, 33, 150], 2
+    r = upload(make(n, n, H, 32, 22, "bf16", seed=46))
+    packs = [gt.gt_attn_pack(n, H, device=DEV)]
+    packs.append(copy.deepcopy(packs[0]))
+
+    def step(pack):
+        args = (r["q"], r["k"], r["v"], r["spd"], r["table"], pack)
+        o, lse = gt.gt_attn_pack_fwd(*args)
+        return o, lse, *gt.gt_attn_pack_bwd(*args, o, lse, r["do"])
+
+    want = step(packs.pop(0))
+    got = step(packs[0])
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("n_k", [[40, 60], [40, 200]])
+def test_keys_without_any_row(dt, n_k):
+    """A batch without query rows whose graphs have keys: zero gradients."""
+    H, d = 2, 16
+    td = torch.bfloat16 if dt == "bf16" else torch.float32
+    k = torch.randn(H, sum(n_k), d, device=DEV).to(td)
+    q, t, spd = k[:, :0].contiguous(), torch.randn(H, 9, device=DEV), torch.zeros(0, dtype=torch.uint8, device=DEV)
+    pack = gt.gt_attn_pack([0, 0], H, n_k=n_k, device=DEV)
+    o, lse = gt.gt_attn_pack_fwd(q, k, k, spd, t, pack, cap=4.0, dropout=DROP)
+    g = gt.gt_attn_pack_bwd(q, k, k, spd, t, pack, o, lse, q, cap=4.0, dropout=DROP)
+    torch.cuda.synchronize()
+    assert o.shape == q.shape and lse.shape == (H, 0) and g[1].shape == k.shape
+    assert all(bool((x == 0).all()) for x in g)
