@@ -444,8 +444,8 @@ gt_status_t gt_attn_pack_fwd(const gt_attn_pack_t* pack, const void* plan, const
  *   dQ = scale dU K,  dK = scale dU^T Q,
  *   dtable[h, b] = sum of dS over pairs with spd == b
  *   dq as q, dk, dv as k (overwritten); dtable [H, n_buckets] fp32 (overwritten).
- * The table gradient is exact to fp32 for bf16 inputs too (the row sums are
- * corrected for the rounding of O). If a dS of a head is no finite number, its whole
+ * The table gradient has fp32's precision for bf16 inputs too (the row sums are
+ * corrected for the rounding of O; with a cap it is off by some 1e-6 of its norm). If a dS of a head is no finite number, its whole
  * dtable row is NaN. Deterministic, the table gradient included. */
 gt_status_t gt_attn_pack_bwd(const gt_attn_pack_t* pack, const void* plan, const gt_attn_rows_t* q,
                              const gt_attn_rows_t* k, const gt_attn_rows_t* v, const uint8_t* spd,

@@ -19,8 +19,11 @@
 //
 // Bound: issue of the element work, some 10 vector instructions per pair and lane with
 // a cap, 3 of them transcendental, against 8 products per block of 32 x 32 at d = 64:
-// vector units busy 80 % (16384 nodes, H = 8, d = 64, cap: 1020 us, 538 TFLOP/s), 98 %
-// with dropout (512 graphs of 100 to 256 nodes, d = 8: 65 us). 16 graphs'
+// vector units busy 80 % (16384 nodes, H = 8, d = 64, cap: 988 us, 556 TFLOP/s), 98 %
+// with dropout (512 graphs of 100 to 256 nodes, d = 8: 67 us), 87 to 89 % at d = 32 and 8
+// with a cap; 63 % where 480 workgroups leave units with one (7651 nodes, dropout: 268 us);
+// fp32: matrix cores 38 %, vector units 34 % at 1.8 waves per SIMD (6 graphs of 300 to 1200,
+// H = 4, d = 32, cap: 40 us). 16 graphs'
 // new node against all their keys: the bytes of K and V, 183 MB in 32 us.
 #pragma once
 #include "pack.hpp"

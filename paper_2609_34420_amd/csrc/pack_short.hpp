@@ -22,10 +22,10 @@
 // fp32 with an error of 2^-22 at least, fp16's step at the low end).
 //
 // Bound: set-up and latency of jobs of one or two blocks, and issue (vector units busy
-// 68 %, with a third or half of the lanes past their graph): 1024 graphs of 9 to 60
-// nodes, H = 8, d = 8, cap: 30 us, where dQ and dK / dV took 25 and 31; 4000 of 50
-// to 64: 144; 2048 of 16 to 40 at d = 64, 256 buckets: 163 for 206; 2048 of 85 to 92 at
-// d = 16, cap: 300 for 390. Longer graphs keep the two passes: their P and dP do not fit
+// 74 %, with a third or half of the lanes past their graph): 1024 graphs of 9 to 60
+// nodes, H = 8, d = 8, cap: 31 us. The whole backward, for that of two passes: those 41 for
+// 63; 4000 of 50 to 64: 172 for 269; 2048 of 16 to 40 at d = 64, 256 buckets: 185 for 238;
+// 2048 of 85 to 92 at d = 16, cap: 296 for 348. Longer graphs keep the two passes: their P and dP do not fit
 // a wave's registers, and D from O is not exact enough for the table gradient. A job's
 // record read a job ahead gained 1 %.
 #pragma once

@@ -130,9 +130,12 @@ def gt_attn_pack(n_q, H: int, n_k=None, prefix=None, spd_off=None, spd_ld=None, 
     default one matrix of n_q[g] rows of the stride behind the other) and their row
     stride (n_k[g]).
     backward=False: a plan for the forward alone, sooner made where a few rows meet
-    many keys (the new nodes of 16 graphs of 1000 to 16000: 45 us for 215). Made
+    many keys (the new nodes of 16 graphs of 1000 to 16000: 40 us for 65). Made
     once per batch of sizes, it serves every layer's and step's calls; a captured
-    graph reads it at each replay, so it has to live as long."""
+    graph reads it at each replay, so it has to live as long, and keeps to its sizes.
+    The copy to the device waits for what the current stream still has to do, and is
+    complete on return: a plan made under a stream of its own does not wait for the
+    queue of another, and may be used on any."""
     nq = _sizes(n_q, "n_q", None)
     nk = nq if n_k is None else _sizes(n_k, "n_k", nq.size)
     opt = [None if x is None else _sizes(x, name, nq.size, t)
@@ -341,7 +344,7 @@ def gt_attn_pack_bwd(q, k, v, spd, table, pack: GTPack, o, lse, d_o, scale: floa
     dv, dtable); rows behind the batch's totals stay as they are. stream: as the
     forward's."""
     if stream is not None:
-        return _on_stream(stream, q, grads or [None] * 4, lambda: gt_attn_pack_bwd(
+        return _on_stream(stream, q, (None,) * 4 if grads is None else grads, lambda: gt_attn_pack_bwd(
             q, k, v, spd, table, pack, o, lse, d_o, scale, cap, dropout, workspace, grads))
     dt, H, d, dev, rows, scale, cap = _common(q, k, v, spd, table, pack, scale, cap)
     T, nb = q.shape[1], table.shape[1]
