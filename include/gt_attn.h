@@ -400,8 +400,9 @@ typedef struct {
  *   prefix    [n_graphs] >= 0, or NULL: no prefix mask
  *   spd_off, spd_ld  [n_graphs] byte offset of a graph's [n_q, n_k] distances and
  *             their row stride (n_k .. 2^25 - 16), or NULL: the rows lie dense, and the
- *             matrices, n_q rows of the stride each, one behind the other. A graph without queries or without keys has no distances:
- *             nothing is read from the place given for it
+ *             matrices, n_q rows of the stride each, one behind the other. A graph without
+ *             queries or without keys has no distances: nothing is read from the place
+ *             given for it
  *   backward  0: without the backward's work lists, for evaluation and serving (they are
  *             most of a plan where a few rows meet many keys)
  *   plan      NULL: only *info is filled; else host memory of plan_bytes bytes that
@@ -445,8 +446,8 @@ gt_status_t gt_attn_pack_fwd(const gt_attn_pack_t* pack, const void* plan, const
  *   dtable[h, b] = sum of dS over pairs with spd == b
  *   dq as q, dk, dv as k (overwritten); dtable [H, n_buckets] fp32 (overwritten).
  * The table gradient has fp32's precision for bf16 inputs too (the row sums are
- * corrected for the rounding of O; with a cap it is off by some 1e-6 of its norm). If a dS of a head is no finite number, its whole
- * dtable row is NaN. Deterministic, the table gradient included. */
+ * corrected for the rounding of O; with a cap it is off by some 1e-6 of its norm). If a
+ * dS of a head is no finite number, its whole dtable row is NaN. Deterministic, the table gradient included. */
 gt_status_t gt_attn_pack_bwd(const gt_attn_pack_t* pack, const void* plan, const gt_attn_rows_t* q,
                              const gt_attn_rows_t* k, const gt_attn_rows_t* v, const uint8_t* spd,
                              const float* table, int32_t n_buckets, const gt_attn_rows_t* o,

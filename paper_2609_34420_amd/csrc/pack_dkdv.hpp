@@ -25,7 +25,8 @@
 // Bound: dependent chains (LDS reads, product, exponentials, product, LDS adds) at two
 // waves per SIMD, which the registers leave at d = 64 (253 of 256): vector units busy
 // 62 %, LDS 19 % (16384 nodes, H = 8, d = 64, cap: 1960 to 2100 us, 530 to 560 TFLOP/s;
-// without the histogram's adds 1840); at three 74 % and 19 % (d <= 32). Two buffers of tiles spill: 2180 against 2115.
+// without the histogram's adds 1840); at three 74 % and 19 % (d <= 32). Two buffers of tiles
+// spill: 2180 against 2115.
 #pragma once
 #include "pack.hpp"
 

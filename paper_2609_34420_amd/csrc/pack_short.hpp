@@ -25,9 +25,9 @@
 // 74 %, with a third or half of the lanes past their graph): 1024 graphs of 9 to 60
 // nodes, H = 8, d = 8, cap: 31 us. The whole backward, for that of two passes: those 41 for
 // 63; 4000 of 50 to 64: 172 for 269; 2048 of 16 to 40 at d = 64, 256 buckets: 185 for 238;
-// 2048 of 85 to 92 at d = 16, cap: 296 for 348. Longer graphs keep the two passes: their P and dP do not fit
-// a wave's registers, and D from O is not exact enough for the table gradient. A job's
-// record read a job ahead gained 1 %.
+// 2048 of 85 to 92 at d = 16, cap: 296 for 348. Longer graphs keep the two passes: their
+// P and dP do not fit a wave's registers, and D from O is not exact enough for the table
+// gradient. A job's record read a job ahead gained 1 %.
 #pragma once
 #include "pack.hpp"
 
